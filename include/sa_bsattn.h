@@ -320,6 +320,145 @@ SA_API int sa_bsattn_plan_stats(sa_plan_t plan, int64_t* executed_blocks);
 /* Frees the plan (hipFree, which waits for outstanding work on the device). */
 SA_API int sa_bsattn_plan_destroy(sa_plan_t plan);
 
+/*
+ * Operators around the attention: what makes its queries and keys, what chooses
+ * its blocks, its gradients, and its form for single tokens.  None allocates,
+ * synchronises or keeps anything: workspaces are the caller's, 256-byte aligned,
+ * of the size that the _workspace function gives (0 for sizes that the call
+ * refuses), need no initial values, and are free again when the call's work on
+ * its stream is done.  Calls that overlap in time need workspaces of their own;
+ * every call may be captured into a graph, whose replays need theirs.  The same
+ * call gives the same bits: no sum goes by the order of arrival.
+ * Strides count elements; they are whole multiples of 8, not negative (0 repeats
+ * a row), and head-dim elements are contiguous.
+ */
+
+/* Which elements a rotation turns together. */
+#define SA_PAIRS_INTERLEAVED 0 /* 2 i and 2 i + 1 */
+#define SA_PAIRS_HALVES 1      /* i and i + rot / 2 */
+
+/*
+ * RMS norm of every head's queries and keys and the rotation by position, from a
+ * projection's output to the tensors that the attention reads (Sec. 4.3.2's
+ * q and k).  For a row x of d elements, w = wq or wk:
+ *   y = x / sqrt(mean x^2 + eps) * w;
+ * the first rot elements are then turned in pairs (a, b) by the angle of the
+ * token's position: (a cos - b sin, a sin + b cos).
+ * q: bf16 [B][N][Hq][d] and k [B][N][Hk][d] with strides {batch, token, head},
+ * 16-byte aligned (so the two may be parts of one projection's rows); wq, wk:
+ * float32 [d]; cos, sin: float32 [n_pos][rot / 2], 16-byte aligned; positions:
+ * int32 [B][N], entries clamped to [0, n_pos), or NULL: token n is at position n
+ * (then n_pos >= N).  q_out, k_out: bf16, contiguous [B][H][N][d] or
+ * [B][N][H][d] by `layout`, rounded once from fp32.  d in {64, 128}; rot a
+ * multiple of 16 up to d; eps >= 0.  Outputs must not overlap inputs or each
+ * other.
+ */
+SA_API int sa_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k,
+                           const int64_t* k_strides, const float* wq, const float* wk,
+                           const float* cos, const float* sin, const int32_t* positions,
+                           void* q_out, void* k_out, int B, int N, int Hq, int Hk, int d, int rot,
+                           int n_pos, float eps, int pairs, int layout, void* stream);
+
+/*
+ * Its gradients.  dq_out, dk_out: bf16 in the layout of q_out and k_out; the
+ * other inputs as there.  dq: bf16 contiguous [B][N][Hq][d], dk [B][N][Hk][d];
+ * dwq, dwk: float32 [d], sums over all tokens and heads.
+ */
+SA_API size_t sa_qk_norm_rope_bwd_workspace(int d);
+
+SA_API int sa_qk_norm_rope_bwd(const void* dq_out, const void* dk_out, const void* q,
+                               const int64_t* q_strides, const void* k, const int64_t* k_strides,
+                               const float* wq, const float* wk, const float* cos,
+                               const float* sin, const int32_t* positions, void* dq, void* dk,
+                               float* dwq, float* dwk, void* workspace, int B, int N, int Hq, int Hk,
+                               int d, int rot, int n_pos, float eps, int pairs, int layout,
+                               void* stream);
+
+/*
+ * Means of blocks of tokens: x bf16 [B][H][N][d] with strides {batch, head,
+ * token}, 16-byte aligned; means float32 [B][H][ceil(N / blk)][d], 16-byte
+ * aligned, the last block's over the tokens it has.  Summed in 64 bits, rounded
+ * once.  d and blk in {64, 128}.
+ */
+SA_API int sa_block_means(const void* x, const int64_t* x_strides, float* means, int B, int H, int N,
+                          int d, int blk, void* stream);
+
+/*
+ * Selection of key blocks by the products of means: row (b, h, u) of mask_bits
+ * (as everywhere, but with one mask for every batch entry: [B][H][n_qb][W])
+ * holds the topk candidates v of largest <q_means[b][h][u], k_means[b][h][v]>,
+ * computed in 64 bits, ties to the lowest v (NaN ranks below everything), all
+ * candidates where there are no more than topk, and every block of keep.
+ * candidates, keep: mask bits [H][n_qb][W] (candidate_batches, keep_batches = 1)
+ * or [B][H][n_qb][W] (= B), or NULL (the counts then don't matter): all blocks
+ * are candidates, nothing is kept beside them.  counts and lists, both or
+ * neither NULL: int32 [B H n_qb] and [B H n_qb][n_kb], the rows' blocks as
+ * sa_mask_prepass gives them.  q_means, k_means: 16-byte aligned.  topk >= 1;
+ * n_kb <= 16384; d in {64, 128}.
+ */
+SA_API int sa_block_select(const float* q_means, const float* k_means, const uint64_t* candidates,
+                           int candidate_batches, const uint64_t* keep, int keep_batches,
+                           uint64_t* mask_bits, int32_t* counts, int32_t* lists, int B, int H,
+                           int n_qb, int n_kb, int d, int topk, void* stream);
+
+/*
+ * Attention over blocks that the means select: sa_block_means of q and k,
+ * sa_block_select of them, and the attention over the selection, whose mask
+ * [B][H][n_qb][W] is an output too.  out and lse are bit for bit those of
+ * sa_bsattn_fwd with B H heads, one batch entry and that mask.
+ */
+SA_API size_t sa_selected_attn_workspace(int B, int H, int N, int d, int blk_q, int blk_k);
+
+SA_API int sa_selected_attn_fwd(const void* q, const void* k, const void* v,
+                                const uint64_t* candidates, int candidate_batches,
+                                const uint64_t* keep, int keep_batches, void* out, float* lse,
+                                uint64_t* mask_bits, void* workspace, int B, int H, int N, int d,
+                                int blk_q, int blk_k, int topk, float scale, void* stream);
+
+/*
+ * Gradients of the attention (Sec. 4.3.2's operation) with the mask held fixed:
+ * with P_ij = exp(s_ij - lse_i) on the pairs of the mask and D_i = <dout_i,
+ * out_i>,
+ *   dv_j = sum_i P_ij dout_i,    dS_ij = P_ij (<dout_i, v_j> - D_i),
+ *   dq_i = scale sum_j dS_ij k_j,    dk_j = scale sum_i dS_ij q_i.
+ * out, lse: of the forward pass with the same arguments.  mask_bits:
+ * [H][n_qb][W] (mask_batches = 1) or [B][H][n_qb][W] (= B).  dout, q, k, v, out,
+ * dq, dk and dv are bf16 in `layout`; lse is [B][H][N].  Query blocks with no set
+ * bit get dq = 0, key blocks that no row enables dk = dv = 0.  P and dS are
+ * rounded to bf16 for the products, everything else is fp32.
+ */
+SA_API size_t sa_bsattn_bwd_workspace(int B, int H, int N, int d, int blk_q, int blk_k,
+                                      int mask_batches);
+
+SA_API int sa_bsattn_bwd(const void* dout, const void* q, const void* k, const void* v,
+                         const void* out, const float* lse, const uint64_t* mask_bits,
+                         int mask_batches, void* dq, void* dk, void* dv, void* workspace, int B,
+                         int H, int N, int d, int blk_q, int blk_k, float scale, int layout,
+                         void* stream);
+
+/*
+ * Attention of one query token a sequence over selected blocks of its cache.
+ * Sequence b has lengths[b] tokens (clamped to [0, cap]), the newest of them the
+ * query's own, in blocks of blk; head h of q reads key head h / (Hq / Hkv).  For
+ * each sequence and key head the newest token's block is taken, and of those
+ * before it, which are complete, the topk - 1 with the largest <means, sum of the
+ * group's queries> (64 bits; ties to the lowest block; all where there are no
+ * more).  out and lse: attention over the tokens of those blocks; a sequence
+ * without tokens gets out = 0 and lse = -inf.
+ * q, out: bf16 [B][Hq][d]; k, v: bf16 [B][Hkv][cap][d] with strides {batch, head,
+ * token}, both alike; means: float32 [B][Hkv][ceil(cap / blk)][d], of the
+ * complete blocks (sa_block_means; others are not read); lengths: int32 [B];
+ * lse: float32 [B][Hq]; blocks: int32 [B][Hkv][topk], the blocks taken, ascending,
+ * then -1.  Tokens past lengths[b] are not read.  d, blk in {64, 128};
+ * ceil(cap / blk) <= 16384.
+ */
+SA_API size_t sa_selected_decode_workspace(int B, int Hq, int Hkv, int cap, int d, int blk, int topk);
+
+SA_API int sa_selected_decode(const void* q, const void* k, const void* v, const int64_t* kv_strides,
+                              const float* means, const int32_t* lengths, void* out, float* lse,
+                              int32_t* blocks, void* workspace, int B, int Hq, int Hkv, int cap,
+                              int d, int blk, int topk, float scale, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,8 @@ work), written to be checked against the paper by eye:
                    of threshold-map masks on sampled rows (Sec. 4.2.3).
 * ``resize``     -- conservative bilinear-ceiling resize of masks and threshold
                    maps between resolutions (Sec. 4.3.1, Eq. 7).
+* ``operators``  -- what stands around the attention: norm and rotation of q and k,
+                   selection of blocks, gradients, single tokens over a cache.
 * ``attention``  -- softmax attention restricted to the key blocks a query
                    block's CRM row enables (Sec. 4.3.2; mask instantiation
                    M_p = 1[T <= p] of Sec. 4.1.2 supplies the masks).

@@ -19,12 +19,16 @@ SA_ERR_HIP = 3
 SA_ERR_TOO_LARGE = 4
 SA_LAYOUT_BHND = 0
 SA_LAYOUT_BNHD = 1
+SA_PAIRS_INTERLEAVED = 0
+SA_PAIRS_HALVES = 1
 
 _LIB = None
 
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
+_Z = ctypes.c_size_t
+_S = ctypes.POINTER(ctypes.c_int64)  # element strides
 
 # name -> (restype, argtypes); mirrors include/sa_bsattn.h
 SIGNATURES = {
@@ -48,6 +52,22 @@ SIGNATURES = {
     "sa_resize_threshold_map": (_I, [_P, _I, _I, _I, _P, _I, _I, _P]),
     "sa_fidelity_profile": (_I, [_P, _P, _P, _I, _P, _P, _I, _P, _P, _P, _I, _I, _I, _I, _I, _F,
                                  _P]),
+    "sa_qk_norm_rope": (_I, [_P, _S, _P, _S, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I,
+                             _F, _I, _I, _P]),
+    "sa_qk_norm_rope_bwd_workspace": (_Z, [_I]),
+    "sa_qk_norm_rope_bwd": (_I, [_P, _P, _P, _S, _P, _S, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I,
+                                 _I, _I, _I, _I, _I, _I, _F, _I, _I, _P]),
+    "sa_block_means": (_I, [_P, _S, _P, _I, _I, _I, _I, _I, _P]),
+    "sa_block_select": (_I, [_P, _P, _P, _I, _P, _I, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P]),
+    "sa_selected_attn_workspace": (_Z, [_I, _I, _I, _I, _I, _I]),
+    "sa_selected_attn_fwd": (_I, [_P, _P, _P, _P, _I, _P, _I, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I,
+                                  _I, _F, _P]),
+    "sa_bsattn_bwd_workspace": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
+    "sa_bsattn_bwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _F,
+                           _I, _P]),
+    "sa_selected_decode_workspace": (_Z, [_I, _I, _I, _I, _I, _I, _I]),
+    "sa_selected_decode": (_I, [_P, _P, _P, _S, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I,
+                                _F, _P]),
 }
 
 
@@ -455,3 +475,330 @@ class Plan:
             self.close()
         except Exception:
             pass
+
+
+# ------------------------------------------------- around the attention ---
+#
+# Tensors may be on any GPU, all on the same one; the work goes to that GPU's
+# current stream, or to ``stream``, which has to be of that GPU.
+
+_PAIRS = {"interleaved": SA_PAIRS_INTERLEAVED, "halves": SA_PAIRS_HALVES}
+_LAYOUTS = {"bhnd": SA_LAYOUT_BHND, "bnhd": SA_LAYOUT_BNHD}
+
+
+def _named(table, key, name):
+    _need(key in table, "%s must be one of %s, got %r" % (name, ", ".join(sorted(table)), key))
+    return table[key]
+
+
+def _tensors(**named):
+    """Type and device checks of the arguments; None stands for one that is left out."""
+    torch = _torch()
+    device = None
+    for name, t in named.items():
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch tensor" % name)
+        if t.device.type != "cuda":
+            raise ValueError("%s must be on the GPU, got %s" % (name, t.device))
+        device = t.device if device is None else device
+        _need(t.device == device, "%s is on %s, others are on %s" % (name, t.device, device))
+    return device
+
+
+def _on(device, stream):
+    """The device made current for the call, whose stream has to be of it."""
+    torch = _torch()
+    _need(stream is None or stream.device == device, "stream is not of device %s" % (device,))
+    return torch.cuda.device(device)
+
+
+def _rows_ptr(t, name):
+    """Pointer and strides of bf16 rows whose last dimension is contiguous; the strides of the
+    others (any order, 0 for a repeated row) in the tensor's order."""
+    torch = _torch()
+    if t.dtype != torch.bfloat16:
+        raise TypeError("%s must be %s, got %s" % (name, torch.bfloat16, t.dtype))
+    _need(t.stride(-1) == 1 or t.shape[-1] == 1, "%s must be contiguous in its last dimension" % name)
+    # the stride of a dimension of one entry means nothing
+    strides = [s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape[:-1])]
+    _need(all(s % 8 == 0 for s in strides) and t.data_ptr() % 16 == 0,
+          "%s: rows must be 16-byte aligned (strides %s)" % (name, tuple(t.stride())))
+    return ctypes.c_void_p(t.data_ptr()), (ctypes.c_int64 * 3)(*strides)
+
+
+def _opt_ptr(t, dtype, name):
+    return None if t is None else _dev_ptr(t, dtype, name)
+
+
+def _workspace(lib, fn, device, *sizes):
+    return _torch().empty(max(1, getattr(lib, fn)(*sizes)), dtype=_torch().uint8, device=device)
+
+
+def _mask_arg(m, B, H, n_qb, n_kb, name):
+    """int64 bits [H, n_qb, W] or [1 or B, H, n_qb, W]; returns (tensor, its batches)."""
+    torch = _torch()
+    if m is None:
+        return None, 1
+    if m.dtype == torch.uint64:
+        m = m.view(torch.int64)
+    shape = (H, n_qb, (n_kb + 63) // 64)
+    batches = m.shape[0] if m.dim() == 4 else 1
+    _need(tuple(m.shape[-3:]) == shape and m.dim() in (3, 4) and batches in (1, B),
+          "%s has shape %s, expected %s, alone or for each batch entry" % (name, tuple(m.shape), shape))
+    return m, batches
+
+
+def _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs, layout):
+    _need(q.dim() == 4 and k.dim() == 4, "q and k must be [B, N, heads, d]")
+    B, N, Hq, d = q.shape
+    Hk = k.shape[2]
+    _need(tuple(k.shape) == (B, N, Hk, d), "k has shape %s, expected [%d, %d, heads, %d]"
+          % (tuple(k.shape), B, N, d))
+    _need(tuple(wq.shape) == (d,) and tuple(wk.shape) == (d,), "wq and wk must be [d]")
+    _need(cos.dim() == 2 and cos.shape == sin.shape, "cos and sin must be [positions, rot / 2]")
+    _need(positions is None or tuple(positions.shape) == (B, N), "positions must be [B, N]")
+    _need(positions is not None or cos.shape[0] >= N, "cos and sin have %d positions for %d tokens"
+          % (cos.shape[0], N))
+    return (B, N, Hq, Hk, d, 2 * cos.shape[1], cos.shape[0], _named(_PAIRS, pairs, "pairs"),
+            _named(_LAYOUTS, layout, "layout"))
+
+
+def _heads_shape(layout, B, N, H, d):
+    return (B, H, N, d) if layout == SA_LAYOUT_BHND else (B, N, H, d)
+
+
+def qk_norm_rope(q, k, wq, wk, cos, sin, positions=None, eps=1e-6, pairs="interleaved",
+                 layout="bhnd", stream=None):
+    """``sa_qk_norm_rope``: every head's RMS norm and the rotation by position.
+
+    q, k: bf16 [B, N, Hq or Hk, d], the first three dimensions of any strides (slices of one
+    projection's output); wq, wk: float32 [d]; cos, sin: float32 [positions, rot / 2];
+    positions: int32 [B, N], None for 0 .. N - 1.  Returns q and k in bf16, [B, H, N, d]
+    (``layout`` "bhnd", as the attention reads them) or [B, N, H, d] ("bnhd").
+    """
+    torch = _torch()
+    device = _tensors(q=q, k=k, wq=wq, wk=wk, cos=cos, sin=sin, positions=positions)
+    B, N, Hq, Hk, d, rot, n_pos, pr, lay = _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs,
+                                                        layout)
+    lib = load()
+    with _on(device, stream):
+        q_out, k_out = (torch.empty(_heads_shape(lay, B, N, H, d), dtype=torch.bfloat16,
+                                    device=device) for H in (Hq, Hk))
+        st = lib.sa_qk_norm_rope(
+            *_rows_ptr(q, "q"), *_rows_ptr(k, "k"), _dev_ptr(wq, torch.float32, "wq"),
+            _dev_ptr(wk, torch.float32, "wk"), _dev_ptr(cos, torch.float32, "cos"),
+            _dev_ptr(sin, torch.float32, "sin"), _opt_ptr(positions, torch.int32, "positions"),
+            _dev_ptr(q_out, torch.bfloat16, "q_out"), _dev_ptr(k_out, torch.bfloat16, "k_out"),
+            B, N, Hq, Hk, d, rot, n_pos, float(eps), pr, lay, _stream(stream))
+        _check("sa_qk_norm_rope", st)
+        _used_on(stream, q_out, k_out)
+    return q_out, k_out
+
+
+def qk_norm_rope_bwd(dq_out, dk_out, q, k, wq, wk, cos, sin, positions=None, eps=1e-6,
+                     pairs="interleaved", layout="bhnd", stream=None):
+    """``sa_qk_norm_rope_bwd``: gradients of ``qk_norm_rope`` with respect to q, k, wq and wk.
+
+    dq_out, dk_out: bf16, contiguous, in the layout of the forward's outputs.  Returns
+    (dq bf16 [B, N, Hq, d], dk bf16 [B, N, Hk, d], dwq float32 [d], dwk float32 [d]).
+    """
+    torch = _torch()
+    device = _tensors(dq_out=dq_out, dk_out=dk_out, q=q, k=k, wq=wq, wk=wk, cos=cos, sin=sin,
+                      positions=positions)
+    B, N, Hq, Hk, d, rot, n_pos, pr, lay = _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs,
+                                                        layout)
+    for t, H, name in ((dq_out, Hq, "dq_out"), (dk_out, Hk, "dk_out")):
+        _need(tuple(t.shape) == _heads_shape(lay, B, N, H, d), "%s has shape %s, expected %s"
+              % (name, tuple(t.shape), _heads_shape(lay, B, N, H, d)))
+    lib = load()
+    with _on(device, stream):
+        dq, dk = (torch.empty((B, N, H, d), dtype=torch.bfloat16, device=device) for H in (Hq, Hk))
+        dwq, dwk = (torch.empty(d, dtype=torch.float32, device=device) for _ in range(2))
+        ws = _workspace(lib, "sa_qk_norm_rope_bwd_workspace", device, d)
+        st = lib.sa_qk_norm_rope_bwd(
+            _dev_ptr(dq_out, torch.bfloat16, "dq_out"), _dev_ptr(dk_out, torch.bfloat16, "dk_out"),
+            *_rows_ptr(q, "q"), *_rows_ptr(k, "k"), _dev_ptr(wq, torch.float32, "wq"),
+            _dev_ptr(wk, torch.float32, "wk"), _dev_ptr(cos, torch.float32, "cos"),
+            _dev_ptr(sin, torch.float32, "sin"), _opt_ptr(positions, torch.int32, "positions"),
+            _dev_ptr(dq, torch.bfloat16, "dq"), _dev_ptr(dk, torch.bfloat16, "dk"),
+            _dev_ptr(dwq, torch.float32, "dwq"), _dev_ptr(dwk, torch.float32, "dwk"),
+            _dev_ptr(ws, torch.uint8, "workspace"), B, N, Hq, Hk, d, rot, n_pos, float(eps), pr,
+            lay, _stream(stream))
+        _check("sa_qk_norm_rope_bwd", st)
+        _used_on(stream, dq, dk, dwq, dwk, ws)
+    return dq, dk, dwq, dwk
+
+
+def block_means(x, blk, stream=None):
+    """``sa_block_means``: float32 [B, H, ceil(N / blk), d], the means of blocks of blk tokens.
+
+    x: bf16 [B, H, N, d], the first three dimensions of any strides (a transposed
+    [B, N, H, d], or the tokens of a cache's newly finished block).
+    """
+    torch = _torch()
+    device = _tensors(x=x)
+    _need(x.dim() == 4, "x must be [B, H, N, d]")
+    B, H, N, d = x.shape
+    _need(blk in (64, 128), "blk must be 64 or 128, got %r" % (blk,))
+    lib = load()
+    with _on(device, stream):
+        means = torch.empty((B, H, -(-N // blk), d), dtype=torch.float32, device=device)
+        st = lib.sa_block_means(*_rows_ptr(x, "x"), _dev_ptr(means, torch.float32, "means"), B, H, N,
+                                d, int(blk), _stream(stream))
+        _check("sa_block_means", st)
+        _used_on(stream, means)
+    return means
+
+
+def block_select(q_means, k_means, topk, candidates=None, keep=None, stream=None):
+    """``sa_block_select``: mask bits int64 [B, H, n_qb, W] of the topk best key blocks of every
+    query block by the products of their means (float32 [B, H, n_qb, d] and [B, H, n_kb, d]).
+
+    candidates: mask bits that choices are limited to; keep: blocks that every row has beside
+    them.  Each int64 [H, n_qb, W], shared by the batch, or [B, H, n_qb, W].
+    """
+    torch = _torch()
+    device = _tensors(q_means=q_means, k_means=k_means, candidates=candidates, keep=keep)
+    _need(q_means.dim() == 4 and k_means.dim() == 4, "q_means and k_means must be [B, H, blocks, d]")
+    B, H, n_qb, d = q_means.shape
+    n_kb = k_means.shape[2]
+    _need(tuple(k_means.shape) == (B, H, n_kb, d), "k_means has shape %s, expected [%d, %d, blocks, %d]"
+          % (tuple(k_means.shape), B, H, d))
+    candidates, cb = _mask_arg(candidates, B, H, n_qb, n_kb, "candidates")
+    keep, kb = _mask_arg(keep, B, H, n_qb, n_kb, "keep")
+    lib = load()
+    with _on(device, stream):
+        mask = torch.empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64, device=device)
+        st = lib.sa_block_select(
+            _dev_ptr(q_means, torch.float32, "q_means"), _dev_ptr(k_means, torch.float32, "k_means"),
+            _opt_ptr(candidates, torch.int64, "candidates"), cb, _opt_ptr(keep, torch.int64, "keep"),
+            kb, _dev_ptr(mask, torch.int64, "mask_bits"), None, None, B, H, n_qb, n_kb, d, int(topk),
+            _stream(stream))
+        _check("sa_block_select", st)
+        _used_on(stream, mask)
+    return mask
+
+
+def selected_attn_fwd(q, k, v, blk_q, blk_k, topk, candidates=None, keep=None, scale=None,
+                      stream=None):
+    """``sa_selected_attn_fwd``: block means of q and k, the selection of ``block_select``, and the
+    attention over it.  q, k, v: bf16 [B, H, N, d].
+
+    Returns (out bf16 [B, H, N, d], lse float32 [B, H, N], mask bits int64 [B, H, n_qb, W]);
+    the mask is what ``bsattn_bwd`` takes.
+    """
+    torch = _torch()
+    device = _tensors(q=q, k=k, v=v, candidates=candidates, keep=keep)
+    _need(q.dim() == 4, "q must be [B, H, N, d]")
+    B, H, N, d = q.shape
+    _same_shape(q, (k, v), ("k", "v"))
+    _need(blk_q in (64, 128) and blk_k in (64, 128), "blk_q and blk_k must be 64 or 128")
+    n_qb, n_kb = -(-N // blk_q), -(-N // blk_k)
+    candidates, cb = _mask_arg(candidates, B, H, n_qb, n_kb, "candidates")
+    keep, kb = _mask_arg(keep, B, H, n_qb, n_kb, "keep")
+    if scale is None:
+        scale = 1.0 / float(d) ** 0.5
+    lib = load()
+    with _on(device, stream):
+        out = torch.empty_like(q)
+        lse = torch.empty((B, H, N), dtype=torch.float32, device=device)
+        mask = torch.empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64, device=device)
+        ws = _workspace(lib, "sa_selected_attn_workspace", device, B, H, N, d, blk_q, blk_k)
+        st = lib.sa_selected_attn_fwd(
+            _dev_ptr(q, torch.bfloat16, "q"), _dev_ptr(k, torch.bfloat16, "k"),
+            _dev_ptr(v, torch.bfloat16, "v"), _opt_ptr(candidates, torch.int64, "candidates"), cb,
+            _opt_ptr(keep, torch.int64, "keep"), kb, _dev_ptr(out, torch.bfloat16, "out"),
+            _dev_ptr(lse, torch.float32, "lse"), _dev_ptr(mask, torch.int64, "mask_bits"),
+            _dev_ptr(ws, torch.uint8, "workspace"), B, H, N, d, int(blk_q), int(blk_k), int(topk),
+            float(scale), _stream(stream))
+        _check("sa_selected_attn_fwd", st)
+        _used_on(stream, out, lse, mask, ws)
+    return out, lse, mask
+
+
+def bsattn_bwd(dout, q, k, v, out, lse, mask_bits, blk_q, blk_k, scale=None, layout="bhnd",
+               stream=None):
+    """``sa_bsattn_bwd``: (dq, dk, dv) of the attention through a block mask held fixed.
+
+    dout, q, k, v, out: bf16 [B, H, N, d], or [B, N, H, d] with ``layout`` "bnhd"; out and lse
+    (float32 [B, H, N]) of the forward pass with the same arguments.  mask_bits: int64 bits
+    [H, n_qb, W] as ``bsattn_fwd`` takes them (numpy too), or [B, H, n_qb, W] as
+    ``selected_attn_fwd`` returns them.
+    """
+    torch = _torch()
+    if not isinstance(mask_bits, torch.Tensor):
+        mask_bits = mask_to_device(mask_bits, q.device)
+    device = _tensors(dout=dout, q=q, k=k, v=v, out=out, lse=lse, mask_bits=mask_bits)
+    lay = _named(_LAYOUTS, layout, "layout")
+    _need(q.dim() == 4, "q must have four dimensions")
+    if lay == SA_LAYOUT_BHND:
+        B, H, N, d = q.shape
+    else:
+        B, N, H, d = q.shape
+    _same_shape(q, (dout, k, v, out), ("dout", "k", "v", "out"))
+    _need(tuple(lse.shape) == (B, H, N), "lse must have shape %s" % ((B, H, N),))
+    _need(blk_q in (64, 128) and blk_k in (64, 128), "blk_q and blk_k must be 64 or 128")
+    m, batches = _mask_arg(mask_bits, B, H, -(-N // blk_q), -(-N // blk_k), "mask_bits")
+    if scale is None:
+        scale = 1.0 / float(d) ** 0.5
+    lib = load()
+    with _on(device, stream):
+        dq, dk, dv = (torch.empty_like(q) for _ in range(3))
+        ws = _workspace(lib, "sa_bsattn_bwd_workspace", device, B, H, N, d, blk_q, blk_k, batches)
+        st = lib.sa_bsattn_bwd(
+            _dev_ptr(dout, torch.bfloat16, "dout"), _dev_ptr(q, torch.bfloat16, "q"),
+            _dev_ptr(k, torch.bfloat16, "k"), _dev_ptr(v, torch.bfloat16, "v"),
+            _dev_ptr(out, torch.bfloat16, "out"), _dev_ptr(lse, torch.float32, "lse"),
+            _dev_ptr(m, torch.int64, "mask_bits"), batches, _dev_ptr(dq, torch.bfloat16, "dq"),
+            _dev_ptr(dk, torch.bfloat16, "dk"), _dev_ptr(dv, torch.bfloat16, "dv"),
+            _dev_ptr(ws, torch.uint8, "workspace"), B, H, N, d, int(blk_q), int(blk_k),
+            float(scale), lay, _stream(stream))
+        _check("sa_bsattn_bwd", st)
+        _used_on(stream, m, dq, dk, dv, ws)
+    return dq, dk, dv
+
+
+def selected_decode(q, k, v, means, lengths, topk, blk, scale=None, stream=None):
+    """``sa_selected_decode``: attention of one token a sequence over the topk blocks of its cache
+    that the means of their keys select, the newest token's among them.
+
+    q: bf16 [B, Hq, d]; k, v: bf16 [B, Hkv, cap, d], the first three dimensions of any strides,
+    both alike, the newest token already in them; means: float32 [B, Hkv, ceil(cap / blk), d],
+    right for the blocks before the newest token's; lengths: int32 [B], tokens in the cache.
+    Returns (out bf16 [B, Hq, d], lse float32 [B, Hq], blocks int32 [B, Hkv, topk]).
+    """
+    torch = _torch()
+    device = _tensors(q=q, k=k, v=v, means=means, lengths=lengths)
+    _need(q.dim() == 3 and k.dim() == 4, "q must be [B, Hq, d], k and v [B, Hkv, cap, d]")
+    B, Hq, d = q.shape
+    Hkv, cap = k.shape[1:3]
+    _need(tuple(k.shape) == (B, Hkv, cap, d) and Hkv > 0 and Hq % Hkv == 0,
+          "k has shape %s, q %s" % (tuple(k.shape), tuple(q.shape)))
+    _same_shape(k, (v,), ("v",))
+    _need(blk in (64, 128), "blk must be 64 or 128, got %r" % (blk,))
+    _need(int(topk) >= 1, "topk must be at least 1")
+    _need(tuple(means.shape) == (B, Hkv, -(-cap // blk), d), "means must have shape %s"
+          % ((B, Hkv, -(-cap // blk), d),))
+    _need(tuple(lengths.shape) == (B,), "lengths must be [B]")
+    if scale is None:
+        scale = 1.0 / float(d) ** 0.5
+    k_ptr, strides = _rows_ptr(k, "k")
+    v_ptr, v_strides = _rows_ptr(v, "v")
+    _need(list(strides) == list(v_strides), "k and v must have the same strides")
+    lib = load()
+    with _on(device, stream):
+        out = torch.empty((B, Hq, d), dtype=torch.bfloat16, device=device)
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=device)
+        blocks = torch.empty((B, Hkv, int(topk)), dtype=torch.int32, device=device)
+        ws = _workspace(lib, "sa_selected_decode_workspace", device, B, Hq, Hkv, cap, d, blk, topk)
+        st = lib.sa_selected_decode(
+            _dev_ptr(q, torch.bfloat16, "q"), k_ptr, v_ptr, strides,
+            _dev_ptr(means, torch.float32, "means"), _dev_ptr(lengths, torch.int32, "lengths"),
+            _dev_ptr(out, torch.bfloat16, "out"), _dev_ptr(lse, torch.float32, "lse"),
+            _dev_ptr(blocks, torch.int32, "blocks"), _dev_ptr(ws, torch.uint8, "workspace"), B, Hq,
+            Hkv, cap, d, int(blk), int(topk), float(scale), _stream(stream))
+        _check("sa_selected_decode", st)
+        _used_on(stream, out, lse, blocks, ws)
+    return out, lse, blocks

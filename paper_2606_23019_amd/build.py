@@ -17,7 +17,8 @@ LIB_NAME = "libsa_bsattn.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 ARCH = "gfx950"
 
-SOURCES = ["api.cpp", "prepass.hip", "mask_inst.hip", "fidelity.hip", "resize.hip", "attn_fwd.hip"]
+SOURCES = ["api.cpp", "ops_api.cpp", "prepass.hip", "mask_inst.hip", "fidelity.hip", "resize.hip",
+           "attn_fwd.hip", "norm_rope.hip", "select.hip", "decode.hip", "attn_bwd.hip"]
 # sustained MFMA rate probe, a measurement helper of bench.py (not in the C ABI)
 MFMA_PEAK_SOURCES = ["mfma_peak.hip"]
 MFMA_PEAK_PATH = os.path.join(PKG_DIR, "libsa_mfma_peak.so")

@@ -1,0 +1,375 @@
+// Attention of one query token a sequence over the blocks of its cache that a cheap
+// score selects.
+//
+// For sequence b of length L (blocks 0 .. last, last = ceil(L / blk) - 1) and key head
+// h, whose group holds G query heads:
+//   score_v = <means_v, sum of the group's q>,  v < last   (64 bits, as in select.hip)
+//   chosen  = the topk - 1 best of them (ties: the lowest v), and block last;
+//   out, lse = softmax attention of the group's G queries over the tokens < L of the
+//              chosen blocks.
+//
+// Two or three launches: decode_select_kernel writes the chosen blocks in ascending
+// order, decode_attn_kernel walks them in `parts` runs, decode_merge_kernel puts the
+// runs together where there is more than one.
+//
+// Bound: HBM bytes of the means and of the chosen blocks' keys and values, which are
+// read once for the whole group; with few rows the latency of the launches.
+
+#include <math.h>
+
+#include "device_common.h"
+#include "launch.h"
+#include "topk_border.h"
+
+namespace sa {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.402823466e+38f;
+
+__device__ __forceinline__ int length_of(const DecodeArgs& a, int b) {
+  return min(max(a.lengths[b], 0), a.cap);
+}
+
+// ---- selection: a workgroup a (sequence, key head) ----
+// Eight lanes take a block's mean, so a wavefront scores eight blocks at a time.
+constexpr int kDecodeSelectThreads = 512;
+
+template <int D>
+__global__ __launch_bounds__(kDecodeSelectThreads) void decode_select_kernel(DecodeArgs a) {
+  extern __shared__ uint64_t keys[];  // [n_blk]
+  __shared__ double qsum[D];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bh = blockIdx.x;
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int G = a.Hq / a.Hkv;
+  const int n = (length_of(a, b) + a.blk - 1) / a.blk;  // blocks with a token
+  const int last = n - 1;
+  int32_t* list = a.blocks + (int64_t)bh * a.topk;
+  if (last + 1 > a.topk) {  // more blocks than are taken: score and choose
+    if (threadIdx.x < D) {
+      const __bf16* q = (const __bf16*)a.q + ((int64_t)b * a.Hq + (int64_t)h * G) * D + threadIdx.x;
+      double t = 0.0;
+      for (int i = 0; i < G; ++i) t += (double)(float)q[(int64_t)i * D];
+      qsum[threadIdx.x] = t;
+    }
+    __syncthreads();
+    const int part = lane & 7;  // columns 4 part + 32 i .. + 3
+    const float* means = a.means + (int64_t)bh * a.n_blk * D + 4 * part;
+    for (int v0 = wave * 8; v0 < last; v0 += kDecodeSelectThreads / 64 * 8) {
+      const int v = v0 + (lane >> 3);
+      const float* m = means + (int64_t)min(v, last - 1) * D;
+      f32x4 x[D / 32];
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) x[i] = *(const f32x4*)(m + 32 * i);
+      double t = 0.0;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t = fma((double)x[i][e], qsum[4 * part + 32 * i + e], t);
+#pragma unroll
+      for (int s = 1; s < 8; s *= 2) t += __shfl_xor(t, s, 64);
+      if (part == 0 && v < last) keys[v] = order_key(t);
+    }
+    __syncthreads();
+  }
+  if (wave != 0) return;
+  int done = 0;
+  if (last + 1 > a.topk) {
+    const int words = (last + 63) / 64;
+    Border edge;
+    if (words <= 4)
+      edge = border_of<4>(keys, last, a.topk - 1, lane);
+    else if (words <= 20)
+      edge = border_of<20>(keys, last, a.topk - 1, lane);
+    else
+      edge = border_of_long(keys, last, a.topk - 1, lane);
+    const uint64_t below = (1ull << lane) - 1ull;
+    for (int w = 0; w < words; ++w) {
+      const uint64_t key = 64 * w + lane < last ? keys[64 * w + lane] : 0;
+      uint64_t word = __ballot(key >= edge.lo);
+      if (edge.ties >= 0) {
+        const uint64_t same = __ballot(key == edge.lo);
+        const bool first = key == edge.lo && (int)__popcll(same & below) < edge.ties;
+        word = __ballot(key > edge.lo || first);
+        edge.ties = max(0, edge.ties - (int)__popcll(same));
+      }
+      if ((word >> lane) & 1ull) list[done + __popcll(word & below)] = 64 * w + lane;
+      done += __popcll(word);
+    }
+    if (lane == 0) list[done] = last;
+    ++done;
+  } else {
+    for (int v = lane; v <= last; v += 64) list[v] = v;
+    done = last + 1;
+  }
+  for (int i = done + lane; i < a.topk; i += 64) list[i] = -1;
+}
+
+// ---- attention ----
+// D = A B + C for a 16 x 16 fp32 tile with K = 32 bf16: lane l supplies
+// A[l % 16][8 (l / 16) + e] and B[8 (l / 16) + e][l % 16], and holds
+// C[4 (l / 16) + i][l % 16].
+__device__ __forceinline__ f32x4 mfma16x16x32(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// XOR of the 16-byte chunk index of a value tile's row: rows read together by a
+// transposing read (4 k .. 4 k + 3) differ in chunk pairs.
+template <int D>
+__device__ __forceinline__ int vswz(int r) {
+  if constexpr (D == 128)
+    return ((r & 3) << 2) | ((r >> 2) & 3);
+  else
+    return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+
+constexpr int kDecodeWaves = 4;
+constexpr int kDecodeGroup = 16;  // query heads of a workgroup: one side of an MFMA tile
+
+// A wavefront takes units of 32 keys: S^T = K Q^T with keys straight from memory
+// (16 bytes a lane, rows in the order that leaves its probabilities as the second
+// product's operand), O^T += V^T P^T with the values through LDS and the transposing
+// read.  Keys of the next unit are requested when S is done, its values when this
+// unit's are in LDS.  Each wavefront has its own maximum and sums; they meet in LDS.
+template <int D>
+__global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeArgs a, int parts,
+                                                                        int groups) {
+  constexpr int C = D / 8;        // 16-byte chunks of a row
+  constexpr int R = 64 / C;       // rows of a load
+  constexpr int kVLoads = 32 / R;
+  __shared__ __attribute__((aligned(1024))) __bf16 Vs[kDecodeWaves][32 * D];
+  __shared__ float stats[kDecodeWaves][2][16];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int part = blockIdx.x % parts;
+  const int rest = blockIdx.x / parts;
+  const int hg = rest % groups;
+  const int bh = rest / groups;
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int G = a.Hq / a.Hkv;
+  const int g0 = hg * kDecodeGroup;
+  const int heads = min(kDecodeGroup, G - g0);
+  const int len = length_of(a, b);
+  const int n = (len + a.blk - 1) / a.blk;
+  const int cnt = min(a.topk, n);
+  const int per = (cnt + parts - 1) / parts;
+  const int i0 = min(part * per, cnt), i1 = min(i0 + per, cnt);
+  const int shift = a.blk == 128 ? 2 : 1;  // units of a block: 4 or 2
+  const int units = (i1 - i0) << shift;
+  const const_ints list = constant(a.blocks) + (int64_t)bh * a.topk + i0;
+
+  bf16x8 qf[D / 32];
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    qf[s] = bf16x8{};
+    if (l16 < heads)
+      qf[s] = *(const bf16x8*)((const __bf16*)a.q +
+                               (((int64_t)b * a.Hq + (int64_t)h * G + g0 + l16) * D + 32 * s + 8 * g));
+  }
+  const __bf16* K = (const __bf16*)a.k + b * a.sb + h * a.sh;
+  const __bf16* V = (const __bf16*)a.v + b * a.sb + h * a.sh;
+  const float c_log2 = a.scale * kLog2e;
+
+  auto key0_of = [&](int u) {  // first token of unit u; blocks are below n
+    const int blk = min(max(list[u >> shift], 0), n - 1);
+    return blk * a.blk + ((u & ((1 << shift) - 1)) << 5);
+  };
+  bf16x8 kf[2][D / 32];
+  u32x4 vr[kVLoads];
+  auto load_k = [&](int key0) {  // rows past the sequence repeat its last one
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const __bf16* row =
+          K + (int64_t)min(key0 + 8 * (l16 >> 2) + 4 * t + (l16 & 3), len - 1) * a.sn + 8 * g;
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) kf[t][s] = *(const bf16x8*)(row + 32 * s);
+    }
+  };
+  auto load_v = [&](int key0) {
+#pragma unroll
+    for (int i = 0; i < kVLoads; ++i)
+      vr[i] = *(const u32x4*)(V + (int64_t)min(key0 + i * R + lane / C, len - 1) * a.sn + 8 * (lane % C));
+  };
+
+  f32x4 o[D / 16];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) o[i] = f32x4{};
+  float m_run = -INFINITY, l_run = 0.f;
+  __bf16* vs = Vs[wave];
+  int u = wave;
+  int key0 = 0;
+  if (u < units) {
+    key0 = key0_of(u);
+    load_k(key0);
+    load_v(key0);
+  }
+  for (; u < units; u += kDecodeWaves) {
+    f32x4 s2[2] = {};
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s2[t] = mfma16x16x32(kf[t][s], qf[s], s2[t]);
+    const bool more = u + kDecodeWaves < units;
+    const int key1 = more ? key0_of(u + kDecodeWaves) : key0;
+    if (more) load_k(key1);
+    float x[8];  // key key0 + 8 g + e, query l16
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = key0 + 8 * g + e < len ? s2[e >> 2][e & 3] : -INFINITY;
+      mx = fmaxf(mx, x[e]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c_log2;
+    const float m_new = fmaxf(m_run, mx);
+    // a maximum of -inf (nothing seen yet, or logits of -inf only) weighs nothing
+    const float m_exp = fmaxf(m_new, kLowest);
+    const float alpha = fast_exp2(m_run - m_exp);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i] *= alpha;
+    bf16x8 pf;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = fast_exp2(fmaf(x[e], c_log2, -m_exp));
+      l_run += p;
+      pf[e] = (__bf16)p;
+    }
+#pragma unroll
+    for (int i = 0; i < kVLoads; ++i) {
+      const int r = i * R + lane / C;
+      lds_write_b128(vs + r * D + (((lane % C) ^ vswz<D>(r)) << 3), vr[i]);
+    }
+    if (more) load_v(key1);
+    // the wavefront's own writes and reads of LDS complete in order
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      const int dd = 16 * i + (lane & 3) * 4;
+      const int r0 = 8 * g + (l16 >> 2), r1 = r0 + 4;
+      const bf16x4 lo = lds_read_tr16_b64(vs + r0 * D + (((dd >> 3) ^ vswz<D>(r0)) << 3) + (dd & 7));
+      const bf16x4 hi = lds_read_tr16_b64(vs + r1 * D + (((dd >> 3) ^ vswz<D>(r1)) << 3) + (dd & 7));
+      const bf16x8 vf = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      o[i] = mfma16x16x32(vf, pf, o[i]);
+    }
+    key0 = key1;
+  }
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+
+  // Put the wavefronts together: out = sum_w exp2(m_w - m) O_w over the same sum of l_w.
+  float* os = (float*)Vs[0];  // [wave][query][D / 4 chunks, XOR of the query] of 4 floats
+  static_assert(sizeof(Vs) >= sizeof(float) * kDecodeWaves * 16 * D, "the value tiles hold the sums");
+  __syncthreads();
+  if (g == 0) {
+    stats[wave][0][l16] = m_run;
+    stats[wave][1][l16] = l_run;
+  }
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {  // o[i][e] is column 16 i + 4 g + e of query l16
+    const int ch = (4 * i + g) ^ l16;
+    *(SA_LDS f32x4*)(os + (wave * 16 + l16) * D + 4 * ch) = o[i];
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < heads * (D / 4); c += 64 * kDecodeWaves) {
+    const int qi = c / (D / 4), ch = c % (D / 4);
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kDecodeWaves; ++w) m = fmaxf(m, stats[w][0][qi]);
+    const float m_exp = fmaxf(m, kLowest);
+    float l = 0.f;
+    f32x4 t = {};
+#pragma unroll
+    for (int w = 0; w < kDecodeWaves; ++w) {
+      const float f = fast_exp2(stats[w][0][qi] - m_exp);
+      l = fmaf(f, stats[w][1][qi], l);
+      t += f * *(const SA_LDS f32x4*)(os + (w * 16 + qi) * D + 4 * (ch ^ qi));
+    }
+    const int64_t row = (int64_t)b * a.Hq + (int64_t)h * G + g0 + qi;
+    if (parts == 1) {
+      const float inv = l != 0.f ? 1.0f / l : 0.f;
+      *(bf16x4*)((__bf16*)a.out + row * D + 4 * ch) =
+          bf16x4{(__bf16)(t[0] * inv), (__bf16)(t[1] * inv), (__bf16)(t[2] * inv), (__bf16)(t[3] * inv)};
+      if (ch == 0) a.lse[row] = l != 0.f ? (m + fast_log2(l)) * kLn2 : -INFINITY;
+    } else {
+      *(f32x4*)(a.parts_out + (row * parts + part) * D + 4 * ch) = t;
+      float* ml = a.parts_out + (int64_t)a.B * a.Hq * parts * D + (row * parts + part) * 2;
+      if (ch == 0) {
+        ml[0] = m;
+        ml[1] = l;
+      }
+    }
+  }
+}
+
+// A wavefront a row: its parts' sums, in order.
+template <int D>
+__global__ __launch_bounds__(256) void decode_merge_kernel(DecodeArgs a, int parts) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= (int64_t)a.B * a.Hq) return;
+  const float* ml = a.parts_out + (int64_t)a.B * a.Hq * parts * D + row * parts * 2;
+  const float* po = a.parts_out + row * parts * D;
+  float m = -INFINITY;
+  for (int p = 0; p < parts; ++p) m = fmaxf(m, ml[2 * p]);
+  const float m_exp = fmaxf(m, kLowest);
+  float l = 0.f;
+  float t[D / 64] = {};
+  for (int p = 0; p < parts; ++p) {
+    const float f = fast_exp2(ml[2 * p] - m_exp);
+    l = fmaf(f, ml[2 * p + 1], l);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) t[i] = fmaf(f, po[p * D + lane * (D / 64) + i], t[i]);
+  }
+  const float inv = l != 0.f ? 1.0f / l : 0.f;
+  __bf16* out = (__bf16*)a.out + row * D + lane * (D / 64);
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) out[i] = (__bf16)(t[i] * inv);
+  if (lane == 0) a.lse[row] = l != 0.f ? (m + fast_log2(l)) * kLn2 : -INFINITY;
+}
+
+int head_groups(int Hq, int Hkv) { return (Hq / Hkv + kDecodeGroup - 1) / kDecodeGroup; }
+
+template <int D>
+hipError_t launch_d(const DecodeArgs& a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.B * a.Hkv;
+  const int parts = decode_parts(a.B, a.Hq, a.Hkv, a.n_blk, a.topk);
+  const int groups = head_groups(a.Hq, a.Hkv);
+  const int lds = a.n_blk * 8;
+  if (lds > 60 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void*)decode_select_kernel<D>,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(decode_select_kernel<D>, dim3((unsigned)rows), dim3(kDecodeSelectThreads), lds,
+                     stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(decode_attn_kernel<D>, dim3((unsigned)(rows * groups * parts)),
+                     dim3(64 * kDecodeWaves), 0, stream, a, parts, groups);
+  e = hipGetLastError();
+  if (e != hipSuccess || parts == 1) return e;
+  hipLaunchKernelGGL(decode_merge_kernel<D>, dim3((unsigned)(((int64_t)a.B * a.Hq + 3) / 4)),
+                     dim3(256), 0, stream, a, parts);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk) {
+  const int64_t rows = (int64_t)B * Hkv * head_groups(Hq, Hkv);
+  const int most = topk < n_blk ? topk : n_blk;
+  const int64_t parts = (1024 + rows - 1) / rows;
+  return (int)(parts < most ? parts : most);
+}
+
+hipError_t launch_selected_decode(const DecodeArgs& a, hipStream_t stream) {
+  return a.d == 128 ? launch_d<128>(a, stream) : launch_d<64>(a, stream);
+}
+
+}  // namespace sa

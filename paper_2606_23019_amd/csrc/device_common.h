@@ -18,6 +18,12 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 #define SA_LDS __attribute__((address_space(3)))
 
+// Memory that no kernel writes while this one runs: uniform reads of it are scalar loads,
+// which do not wait behind tile copies.
+#define SA_CONST const __attribute__((address_space(4)))
+typedef SA_CONST int32_t* const_ints;
+__device__ __forceinline__ const_ints constant(const int32_t* p) { return (const_ints)(uintptr_t)p; }
+
 // D = A * B + C for a 32x32 fp32 tile with K = 16 bf16 (v_mfma_f32_32x32x16_bf16).
 // Lane l supplies A[l % 32][8 * (l / 32) + e] and B[8 * (l / 32) + e][l % 32],
 // e = 0..7, and holds C[8 * (i / 4) + 4 * (l / 32) + i % 4][l % 32] in register i.

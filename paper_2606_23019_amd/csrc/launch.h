@@ -29,6 +29,110 @@ struct AttnArgs {
   const uint64_t* mask_bits = nullptr;
 };
 
+// One side (queries or keys) of the norm and rotation: x with element strides of
+// batch, token and head (the head-dim is contiguous), y or its gradient in the
+// output's layout, dx contiguous [B][N][H][d].
+struct RopeSide {
+  const void* x;
+  int64_t sb, sn, sh;
+  const float* w;
+  const void* y;
+  void* dx;
+  int H;
+};
+
+struct RopeArgs {
+  RopeSide t[2];
+  const float* cos;
+  const float* sin;
+  const int32_t* positions;
+  float* dw_parts;  // gradients only: float [kRopeParts][2][d]
+  int B, N, d, rot, n_pos;
+  float eps;
+  bool halves, bhnd;
+  int heads;  // set by the launchers
+};
+
+// Blocks of the gradients' kernel at most, each with its own sums for dw.
+constexpr int kRopeParts = 1024;
+
+hipError_t launch_norm_rope(RopeArgs a, hipStream_t stream);
+hipError_t launch_norm_rope_bwd(RopeArgs a, float* dwq, float* dwk, hipStream_t stream);
+
+hipError_t launch_block_means(const void* x, int64_t sb, int64_t sh, int64_t sn, float* means,
+                              int B, int H, int N, int d, int blk, hipStream_t stream);
+
+// Most key blocks of a row that is selected: its keys have to fit in LDS.
+constexpr int kSelectMaxBlocks = 16384;
+
+struct SelectArgs {
+  const float* qm;
+  const float* km;
+  const uint64_t* candidates;  // or null
+  const uint64_t* keep;        // or null
+  uint64_t* bits;
+  int32_t* counts;  // with lists, or both null
+  int32_t* lists;
+  int B, H, n_qb, n_kb, d, topk;
+  bool cand_per_batch, keep_per_batch;
+};
+
+hipError_t launch_block_select(const SelectArgs& a, hipStream_t stream);
+
+// Single-token attention over selected blocks of a cache.
+struct DecodeArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const float* means;
+  const int32_t* lengths;
+  void* out;
+  float* lse;
+  int32_t* blocks;
+  float* parts_out;  // parts > 1: float [B][Hq][parts][d], then [B][Hq][parts][2]
+  int B, Hq, Hkv, cap, d, blk, n_blk, topk;
+  int64_t sb, sh, sn;  // element strides of k and v: batch, head, token
+  float scale;
+};
+
+// Parts that a row's blocks are walked in, each by a workgroup of its own.
+int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk);
+
+hipError_t launch_selected_decode(const DecodeArgs& a, hipStream_t stream);
+
+// Lists that a kernel walks and the order of its items.
+struct BwdLists {
+  const int32_t* counts;
+  const int32_t* lists;
+  const int32_t* order;
+};
+
+struct BwdArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* out;
+  const void* dout;
+  const float* lse;
+  void* dq;
+  void* dk;
+  void* dv;
+  float* nlse;    // float [B H][n_pad], n_pad = N rounded up to 128
+  float* ndelta;  // the same
+  int B, H, N, d, blk_q, blk_k, n_qb, n_kb, n_pad;
+  int mask_heads;  // H, or B H with a mask for every batch entry
+  float scale;
+  int64_t sb, sh;  // element strides: batch, head, token
+  int sn;
+  float c_log2;  // set by the launcher
+};
+
+hipError_t launch_column_lists(const uint64_t* mask_bits, int H, int n_qb, int n_kb, int32_t* counts,
+                               int32_t* lists, hipStream_t stream);
+
+hipError_t launch_attention_bwd(const BwdArgs& a, const BwdLists& rows, const BwdLists& columns,
+                                hipStream_t stream);
+
 hipError_t launch_prepass(const uint64_t* mask_bits, int H, int n_qb, int n_kb, int32_t* counts,
                           int32_t* lists, hipStream_t stream);
 

@@ -1,0 +1,193 @@
+// Choice of key blocks by a cheap score: means of blocks of tokens, and for every
+// query block the topk key blocks whose mean key has the largest product with its
+// mean query, as a Compressed Row Mask (and as the lists the attention kernel walks).
+//
+//   m_u = (1 / size_u) sum of the block's rows,  score_uv = sum_c qm_uc km_vc,
+//   row u: the topk candidates of largest score (ties: the lowest v), and keep.
+//
+// A choice is a comparison, so the sums are held in 64 bits: neither the order of the
+// sums nor an fp32 rounding decides between two blocks.  A mean is the fp32 rounding
+// of the 64-bit sum's quotient, a score the 64-bit sum of exact products.
+
+#include "device_common.h"
+#include "launch.h"
+#include "topk_border.h"
+
+namespace sa {
+
+namespace {
+
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+// ---- means ----
+// One block of tokens a workgroup, d / 8 lanes a row, each lane 8 columns in 64 bits.
+// Bound by the HBM bytes of x; a block's 8 to 32 KB are requested in one go.
+template <int D, int BLK>
+__global__ __launch_bounds__(256) void block_means_kernel(const __bf16* __restrict__ x, int64_t sb,
+                                                          int64_t sh, int64_t sn,
+                                                          float* __restrict__ means, int H, int N,
+                                                          int n_blk) {
+  constexpr int C = D / 8, R = 256 / C;  // rows a pass
+  __shared__ double sums[4][D];
+  const int64_t item = blockIdx.x;
+  const int64_t bh = item / n_blk;
+  const int blk = (int)(item - bh * n_blk);
+  const int lane = threadIdx.x & 63;
+  const int chunk = threadIdx.x % C;
+  const int size = min(BLK, N - blk * BLK);
+  const __bf16* from = x + (bh / H) * sb + (bh % H) * sh + (int64_t)blk * BLK * sn + 8 * chunk;
+  u32x4 v[BLK / R];
+#pragma unroll
+  for (int i = 0; i < BLK / R; ++i) {
+    const int row = threadIdx.x / C + i * R;
+    v[i] = row < size ? *(const u32x4*)(from + row * sn) : u32x4{};
+  }
+  double t[8] = {};
+#pragma unroll
+  for (int i = 0; i < BLK / R; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      t[2 * e] += (double)__uint_as_float(v[i][e] << 16);
+      t[2 * e + 1] += (double)__uint_as_float(v[i][e] & 0xffff0000u);
+    }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int s = C; s < 64; s *= 2) t[e] += __shfl_xor(t[e], s, 64);
+  if (lane < C)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[threadIdx.x / 64][8 * chunk + e] = t[e];
+  __syncthreads();
+  if (threadIdx.x < D) {
+    const int c = threadIdx.x;
+    means[item * D + c] = (float)((sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c]) / size);
+  }
+}
+
+// ---- selection ----
+constexpr int kSelectLds = 156 * 1024;
+constexpr int kSelectRows = 16;  // rows of a workgroup: one side of an MFMA tile
+
+// Scores of `rows` (up to 16) query blocks against all key blocks by
+// v_mfma_f64_16x16x4, as ordered keys in LDS, then a wavefront a row picks.  Lane l
+// supplies row (or key block) l % 16 and, in step 4 s + e, the column 16 s + 4 (l / 16)
+// + e of both sides, so that its loads are 16 bytes; every key block's sum runs in the
+// same order, so equal blocks score alike.
+template <int D>
+__global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, int rows, int groups) {
+  extern __shared__ uint64_t keys_all[];  // [rows][n_pad]
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = blockDim.x / 64;
+  const int n_pad = (a.n_kb + 15) / 16 * 16;
+  const int bh = blockIdx.x / groups;
+  const int u0 = (blockIdx.x - bh * groups) * rows;
+  const int n_rows = min(rows, a.n_qb - u0);
+  const int l16 = lane & 15, g = lane >> 4;
+
+  const float* qrow = a.qm + ((int64_t)bh * a.n_qb + u0 + min(l16, n_rows - 1)) * D + 4 * g;
+  const float* kmat = a.km + (int64_t)bh * a.n_kb * D + 4 * g;
+  double qa[D / 4];
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const f32x4 v = *(const f32x4*)(qrow + 16 * s);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) qa[4 * s + e] = v[e];
+  }
+  const int h = bh % a.H;
+  const int words = (a.n_kb + 63) / 64;
+  for (int v0 = wave * 16; v0 < a.n_kb; v0 += waves * 16) {
+    const int v = v0 + l16;
+    const float* krow = kmat + (int64_t)min(v, a.n_kb - 1) * D;
+    f32x4 kb[D / 16];
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) kb[s] = *(const f32x4*)(krow + 16 * s);
+    f64x4 c = {};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        c = __builtin_amdgcn_mfma_f64_16x16x4f64(qa[4 * s + e], (double)kb[s][e], c, 0, 0, 0);
+    // register i of lane l holds row 4 i + l / 16 (64-bit tiles interleave rows), key block v
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 4 * i + g;
+      if (row < n_rows) keys_all[row * n_pad + v] = order_key(c[i]);
+    }
+  }
+  __syncthreads();
+  for (int row = wave; row < n_rows; row += waves) {
+    const int64_t at = ((int64_t)bh * a.n_qb + u0 + row);
+    const int64_t shared = ((int64_t)h * a.n_qb + u0 + row);
+    const uint64_t* cand =
+        a.candidates ? a.candidates + (a.cand_per_batch ? at : shared) * words : nullptr;
+    const uint64_t* keep = a.keep ? a.keep + (a.keep_per_batch ? at : shared) * words : nullptr;
+    uint64_t* keys = keys_all + row * n_pad;
+    if (cand)
+      for (int w = 0; w < words; ++w)
+        if (64 * w + lane < a.n_kb && !((cand[w] >> lane) & 1ull)) keys[64 * w + lane] = 0;
+    Border edge;
+    if (words <= 4)
+      edge = border_of<4>(keys, a.n_kb, a.topk, lane);
+    else if (words <= 10)
+      edge = border_of<10>(keys, a.n_kb, a.topk, lane);
+    else if (words <= 20)
+      edge = border_of<20>(keys, a.n_kb, a.topk, lane);
+    else
+      edge = border_of_long(keys, a.n_kb, a.topk, lane);
+    const uint64_t below = (1ull << lane) - 1ull;
+    int done = 0;
+    for (int w = 0; w < words; ++w) {
+      const uint64_t key = 64 * w + lane < a.n_kb ? keys[64 * w + lane] : 0;
+      uint64_t word = __ballot(key >= edge.lo);
+      if (edge.ties >= 0) {
+        const uint64_t same = __ballot(key == edge.lo);
+        const bool first = key == edge.lo && (int)__popcll(same & below) < edge.ties;
+        word = __ballot(key > edge.lo || first);
+        edge.ties = max(0, edge.ties - (int)__popcll(same));
+      }
+      if (keep) {
+        const int real = a.n_kb - 64 * w;
+        word |= keep[w] & (real < 64 ? (1ull << real) - 1ull : ~0ull);
+      }
+      if (lane == 0) a.bits[at * words + w] = word;
+      if (a.counts && ((word >> lane) & 1ull))
+        a.lists[at * a.n_kb + done + __popcll(word & below)] = 64 * w + lane;
+      done += __popcll(word);
+    }
+    if (a.counts && lane == 0) a.counts[at] = done;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_block_means(const void* x, int64_t sb, int64_t sh, int64_t sn, float* means,
+                              int B, int H, int N, int d, int blk, hipStream_t stream) {
+  const int n_blk = (N + blk - 1) / blk;
+  const int64_t grid = (int64_t)B * H * n_blk;
+  auto kernel = d == 128 ? (blk == 128 ? block_means_kernel<128, 128> : block_means_kernel<128, 64>)
+                         : (blk == 128 ? block_means_kernel<64, 128> : block_means_kernel<64, 64>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, (const __bf16*)x, sb, sh,
+                     sn, means, H, N, n_blk);
+  return hipGetLastError();
+}
+
+hipError_t launch_block_select(const SelectArgs& a, hipStream_t stream) {
+  const int n_pad = (a.n_kb + 15) / 16 * 16;
+  int rows = kSelectLds / (n_pad * 8);
+  if (rows < 1) return hipErrorInvalidValue;
+  if (rows > kSelectRows) rows = kSelectRows;
+  const int groups = (a.n_qb + rows - 1) / rows;
+  const int64_t grid = (int64_t)a.B * a.H * groups;
+  const int lds = rows * n_pad * 8;
+  auto kernel = a.d == 128 ? block_select_kernel<128> : block_select_kernel<64>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), lds, stream, a, rows, groups);
+  return hipGetLastError();
+}
+
+}  // namespace sa
