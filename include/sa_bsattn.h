@@ -425,7 +425,8 @@ SA_API int sa_selected_attn_fwd(const void* q, const void* k, const void* v,
  * [H][n_qb][W] (mask_batches = 1) or [B][H][n_qb][W] (= B).  dout, q, k, v, out,
  * dq, dk and dv are bf16 in `layout`; lse is [B][H][N].  Query blocks with no set
  * bit get dq = 0, key blocks that no row enables dk = dv = 0.  P and dS are
- * rounded to bf16 for the products, everything else is fp32.
+ * rounded to bf16 for the products, everything else is fp32.  The masks' rows
+ * have to have fewer than 2^31 bits in all.
  */
 SA_API size_t sa_bsattn_bwd_workspace(int B, int H, int N, int d, int blk_q, int blk_k,
                                       int mask_batches);

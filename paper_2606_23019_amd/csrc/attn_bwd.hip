@@ -53,15 +53,68 @@ __device__ __forceinline__ bf16x8 columns_operand(const __bf16* tile, int r0, in
   return bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
 }
 
-// ---- rows ----
-// D / 8 lanes a row.  rows[bh][n] = {-lse / scale, -D}; past N {-inf, 0}, up to n_pad.
+// ---- preparation: lists of the mask's rows and columns, two floats a row ----
+// One launch of independent blocks: first those of the mask's rows (a wavefront each,
+// the key blocks of (h, u)), then of its columns (the query blocks whose row has bit
+// v), both ascending; then of rows[bh][n] = {-lse / scale, -D}, d / 8 lanes each
+// (past N {-inf, 0}, up to n_pad).
+struct PrepGrid {
+  int row_blocks, column_blocks, token_blocks;
+};
+
 template <int D>
-__global__ __launch_bounds__(256) void bwd_rows_kernel(BwdArgs a) {
+__global__ __launch_bounds__(256) void bwd_prep_kernel(BwdArgs a, PrepGrid grid) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t below = (1ull << lane) - 1ull;
+  const int W = (a.n_kb + 63) / 64;
+  int blk = blockIdx.x;
+  if (blk < grid.row_blocks) {
+    const int64_t row = (int64_t)blk * 4 + wave;
+    if (row >= (int64_t)a.mask_heads * a.n_qb) return;
+    const uint64_t* words = a.mask + row * W;
+    int32_t* list = a.row_lists + row * a.n_kb;
+    int done = 0;
+    for (int w0 = 0; w0 < W; w0 += 64) {
+      // 64 words at a time, handed to the wavefront one by one
+      const int real = a.n_kb - (w0 + lane) * 64;
+      uint64_t mine = w0 + lane < W ? words[w0 + lane] : 0;
+      if (real < 64) mine &= real > 0 ? (1ull << real) - 1ull : 0;
+      for (int i = 0; i < min(64, W - w0); ++i) {
+        const uint64_t word =
+            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, i) |
+            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), i) << 32;
+        if ((word >> lane) & 1ull) list[done + __popcll(word & below)] = (w0 + i) * 64 + lane;
+        done += __popcll(word);
+      }
+    }
+    if (lane == 0) a.row_counts[row] = done;
+    return;
+  }
+  blk -= grid.row_blocks;
+  if (blk < grid.column_blocks) {
+    const int64_t col = (int64_t)blk * 4 + wave;
+    if (col >= (int64_t)a.mask_heads * a.n_kb) return;
+    const int64_t h = col / a.n_kb;
+    const int v = (int)(col - h * a.n_kb);
+    const uint64_t* word = a.mask + h * a.n_qb * W + v / 64;
+    int32_t* list = a.column_lists + col * a.n_qb;
+    int done = 0;
+    for (int u0 = 0; u0 < a.n_qb; u0 += 64) {
+      const int u = u0 + lane;
+      const bool on = u < a.n_qb && ((word[(int64_t)min(u, a.n_qb - 1) * W] >> (v & 63)) & 1ull);
+      const uint64_t all = __ballot(on);
+      if (on) list[done + __popcll(all & below)] = u;
+      done += __popcll(all);
+    }
+    if (lane == 0) a.column_counts[col] = done;
+    return;
+  }
+  blk -= grid.column_blocks;
   constexpr int C = D / 8, R = 256 / C;
-  const int64_t blocks = (a.n_pad + R - 1) / R;
-  const int64_t bh = blockIdx.x / blocks;
-  const int n = (int)(blockIdx.x - bh * blocks) * R + threadIdx.x / C;
-  if (n >= a.n_pad) return;
+  const int blocks = a.n_pad / R;
+  const int64_t bh = blk / blocks;
+  const int n = (blk - (int)bh * blocks) * R + threadIdx.x / C;
   float t = 0.f;
   if (n < a.N) {
     const int64_t at = (bh / a.H) * a.sb + (bh % a.H) * a.sh + (int64_t)n * a.sn + 8 * (threadIdx.x % C);
@@ -78,61 +131,203 @@ __global__ __launch_bounds__(256) void bwd_rows_kernel(BwdArgs a) {
   }
 }
 
-// ---- lists of a mask's columns ----
-// A wavefront a column (h, v): the query blocks whose row has bit v, ascending.
-__global__ __launch_bounds__(256) void column_lists_kernel(const uint64_t* __restrict__ mask,
-                                                           int64_t columns, int n_qb, int n_kb,
-                                                           int32_t* __restrict__ counts,
-                                                           int32_t* __restrict__ lists) {
-  const int lane = threadIdx.x & 63;
-  const int64_t col = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (col >= columns) return;
-  const int64_t h = col / n_kb;
-  const int v = (int)(col - h * n_kb);
-  const int W = (n_kb + 63) / 64;
-  const uint64_t* word = mask + h * n_qb * W + v / 64;
-  int done = 0;
-  for (int u0 = 0; u0 < n_qb; u0 += 64) {
-    const int u = u0 + lane;
-    const bool on = u < n_qb && ((word[(int64_t)min(u, n_qb - 1) * W] >> (v & 63)) & 1ull);
-    const uint64_t all = __ballot(on);
-    if (on) lists[col * n_qb + done + __popcll(all & ((1ull << lane) - 1ull))] = u;
-    done += __popcll(all);
+// ---- plan ----
+// The workgroups of the two kernels, as tables of (item, first list entry, entries,
+// slot).  An item is a query block's or a key block's list.  Columns that every row sees
+// are many times longer than the mean, and a short problem has fewer items than the chip
+// has places, so
+//   - lists of more than `limit` = max(least, total / places) entries are cut into equal
+//     parts of at most that, which come first; their sums go to slots of the workspace
+//     and bwd_join_kernel adds them up in order;
+//   - the others follow in the XCD layout of the forward kernel's schedule (heads in index
+//     order), inside every XCD's sequence the longest first by coarse classes, so that
+//     long lists do not start last and neighbours still share tiles in L2.
+// Places that stay empty have entries < 0.
+constexpr int kPlaces = 512;            // two workgroups on each of 256 compute units
+constexpr int kFront = 2 * kPlaces;     // parts at most: c > limit makes less than c / limit + 1
+constexpr int kLeast = 2;               // shortest part, in list entries
+constexpr int kClasses = 4;             // of list length: over 2, 1 and 1 / 2 of the mean, others
+
+struct PlanSide {
+  const int32_t* counts;  // [mask_heads][n_own]
+  int4* table;            // [front + n_items rounded up to 8]
+  int4* splits;           // [kPlaces]: item, first slot, parts
+  int32_t* n_splits;
+  int n_own, front, n_items, least;
+};
+
+__global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide columns, int mask_heads,
+                                                        int heads) {
+  __shared__ int sums[1024];
+  __shared__ int class_count[kClasses];
+  const PlanSide& o = blockIdx.y ? columns : rows;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int own = mask_heads * o.n_own;   // counts
+  int t = 0;
+  for (int i = tid; i < own; i += 1024) t += o.counts[i];
+  sums[tid] = t;
+  __syncthreads();
+  for (int s = 512; s > 0; s >>= 1) {
+    if (tid < s) sums[tid] += sums[tid + s];
+    __syncthreads();
   }
-  if (lane == 0) counts[col] = done;
+  // a count of list entries fits 31 bits where its lists fit in memory; the batch may not
+  const int64_t total = (int64_t)sums[0] * (heads / mask_heads);
+  const int limit = (int)max((int64_t)o.least, (total + kPlaces - 1) / kPlaces);
+  const int mean = max(1, sums[0] / own);
+  __syncthreads();
+  auto count_of = [&](int item) {
+    const int bh = item / o.n_own;
+    return o.counts[(int64_t)(bh % mask_heads) * o.n_own + (item - bh * o.n_own)];
+  };
+  if (blockIdx.x == kXcds) {  // the parts, in the order of the items
+    if (o.front == 0) {
+      if (tid == 0) *o.n_splits = 0;
+      return;
+    }
+    const int seg = (o.n_items + 1023) / 1024;
+    const int i0 = min(tid * seg, o.n_items), i1 = min(i0 + seg, o.n_items);
+    int parts = 0, splits = 0;
+    for (int i = i0; i < i1; ++i) {
+      const int c = count_of(i);
+      if (c > limit) {
+        parts += (c + limit - 1) / limit;
+        ++splits;
+      }
+    }
+    sums[tid] = parts | splits << 16;  // both at most kFront
+    __syncthreads();
+    for (int s = 1; s < 1024; s <<= 1) {
+      const int x = tid >= s ? sums[tid - s] : 0;
+      __syncthreads();
+      sums[tid] += x;
+      __syncthreads();
+    }
+    int slot = (sums[tid] & 0xffff) - parts, at = (sums[tid] >> 16) - splits;
+    for (int i = i0; i < i1; ++i) {
+      const int c = count_of(i);
+      if (c <= limit) continue;
+      const int n = (c + limit - 1) / limit;
+      o.splits[at++] = make_int4(i, slot, n, 0);
+      for (int p = 0; p < n; ++p, ++slot) {
+        const int first = (int)((int64_t)p * c / n);
+        o.table[slot] = make_int4(i, first, (int)((int64_t)(p + 1) * c / n) - first, slot);
+      }
+    }
+    const int used = sums[1023] & 0xffff;
+    for (int i = used + tid; i < o.front; i += 1024) o.table[i] = make_int4(0, 0, -1, -1);
+    if (tid == 0) *o.n_splits = sums[1023] >> 16;
+    return;
+  }
+  // sequence x: a wavefront a class, which finds its members' number and then their places
+  const int x = blockIdx.x;
+  const int units = o.n_items / o.n_own;
+  const int len = (o.n_items - x + kXcds - 1) / kXcds;
+  int4* seq = o.table + o.front;
+  auto mine = [&](int j, int* item, int* c) {  // whether place j is of the wavefront's class
+    if (j >= len) return false;
+    int u;
+    const int unit = xcd_slice(x + (int64_t)kXcds * j, units, o.n_own, &u);
+    *item = unit * o.n_own + u;
+    *c = count_of(*item);
+    const int cls = *c > 2 * mean ? 0 : *c > mean ? 1 : 2 * *c > mean ? 2 : 3;
+    return cls == wave && !(o.front && *c > limit);
+  };
+  if (wave < kClasses) {
+    int item = 0, c = 0, n = 0;
+    for (int j = lane; j < len + lane; j += 64) n += __popcll(__ballot(mine(j, &item, &c)));
+    if (lane == 0) class_count[wave] = n;
+  }
+  __syncthreads();
+  int base = 0, all = 0;
+  for (int w = 0; w < kClasses; ++w) {
+    base += w < wave ? class_count[w] : 0;
+    all += class_count[w];
+  }
+  if (wave < kClasses) {
+    for (int j = lane; j < len + lane; j += 64) {
+      int item = 0, c = 0;
+      const bool in = mine(j, &item, &c);
+      const uint64_t on = __ballot(in);
+      if (in) seq[x + kXcds * (base + __popcll(on & ((1ull << lane) - 1ull)))] = make_int4(item, 0, c, -1);
+      base += __popcll(on);
+    }
+  }
+  for (int j = all + tid; x + kXcds * j < (o.n_items + kXcds - 1) / kXcds * kXcds; j += 1024)
+    seq[x + kXcds * j] = make_int4(0, 0, -1, -1);
 }
 
 constexpr int kWalk = 64;  // rows of a walked tile
 
-// An item of a kernel's grid: `own` block of 32 kWaves rows and its list of blocks.
+// A workgroup's part of an item: `own` block of 32 kWaves rows, its list's entries.
 struct Item {
   int64_t bh;
-  int block;
+  int block, cnt, slot;
   const_ints list;
-  int cnt;
 };
 
-__device__ __forceinline__ Item item_of(const BwdArgs& a, const BwdLists& l, int n_own, int n_walked) {
-  const int items = (int)gridDim.x;
-  const int it = min(max(constant(l.order)[blockIdx.x], 0), items - 1);
+__device__ __forceinline__ Item item_of(const BwdArgs& a, const BwdSide& l, int n_own, int n_walked) {
+  typedef SA_CONST i32x4* Entries;
+  const i32x4 e = *((Entries)(uintptr_t)l.table + blockIdx.x);
   Item r;
-  r.bh = it / n_own;
-  r.block = it - (int)r.bh * n_own;
-  const int64_t row = (r.bh % a.mask_heads) * n_own + r.block;
-  r.cnt = min(max(constant(l.counts)[row], 0), n_walked);
-  r.list = constant(l.lists) + row * n_walked;
+  r.bh = e.x / n_own;
+  r.block = e.x - (int)r.bh * n_own;
+  r.cnt = e.z;
+  r.slot = e.w;
+  r.list = constant(l.lists) + ((r.bh % a.mask_heads) * n_own + r.block) * n_walked + e.y;
   return r;
+}
+
+// Accumulators of a part, as they lie in the registers: 16 floats a lane and column group.
+template <int D>
+__device__ __forceinline__ void store_part(const f32x16 (&o)[D / 32], float* at, int lane) {
+#pragma unroll
+  for (int dg = 0; dg < D / 32; ++dg)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *(f32x4*)(at + (dg * 4 + i / 4) * 256 + lane * 4) =
+          f32x4{o[dg][i], o[dg][i + 1], o[dg][i + 2], o[dg][i + 3]};
+}
+
+// Joins the parts of split items: a wavefront 32 rows x 32 columns of one of them.
+template <int D>
+__global__ __launch_bounds__(256) void bwd_join_kernel(BwdArgs a, BwdSide l, int n_own, int blk,
+                                                       int results) {
+  const int per = blk / 32 * (D / 32) * results;  // wavefronts an item
+  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int at = (int)(w / per);
+  if (at >= *l.n_splits) return;
+  const int4 e = l.splits[at];
+  const int unit = (int)(w - (int64_t)at * per);
+  const int dg = unit % (D / 32), rest = unit / (D / 32);
+  const int which = rest % results, rows = rest / results;  // result, group of 32 rows
+  const int lane = threadIdx.x & 63;
+  const float* from = a.parts + ((int64_t)e.y * (blk / 32) * results + rows * results + which) * (32 * D) +
+                      dg * 1024 + lane * 4;
+  f32x4 t[4] = {};
+  for (int p = 0; p < e.z; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] += *(const f32x4*)(from + (int64_t)p * blk * D * results + i * 256);
+  const int64_t bh = e.x / n_own;
+  const int row = (e.x - (int)bh * n_own) * blk + rows * 32 + (lane & 31);
+  if (row >= a.N) return;
+  __bf16* out = (__bf16*)(results == 1 ? a.dq : which ? a.dv : a.dk);
+  const float f = which ? 1.f : a.scale;
+  out += (bh / a.H) * a.sb + (bh % a.H) * a.sh + (int64_t)row * a.sn + dg * 32 + 4 * (lane >> 5);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) store_out4(out + 8 * i, t[i][0] * f, t[i][1] * f, t[i][2] * f, t[i][3] * f);
 }
 
 // ---- dQ ----
 template <int BQ, int D>
-__global__ __launch_bounds__(BQ * 2, 2) void bwd_dq_kernel(BwdArgs a, BwdLists lists) {
+__global__ __launch_bounds__(BQ * 2, 2) void bwd_dq_kernel(BwdArgs a, BwdSide side) {
   using T = Tile<BQ, kWalk, D>;
   __shared__ __attribute__((aligned(1024))) __bf16 tiles[2][2][kWalk * D];  // buffer, K or V
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const Item item = item_of(a, lists, a.n_qb, a.n_kb);
+  const Item item = item_of(a, side, a.n_qb, a.n_kb);
+  if (item.cnt < 0) return;
   const int64_t base = (item.bh / a.H) * a.sb + (item.bh % a.H) * a.sh;
   const __bf16* Kb = (const __bf16*)a.k + base - kCopyShift;
   const __bf16* Vb = (const __bf16*)a.v + base - kCopyShift;
@@ -205,54 +400,87 @@ __global__ __launch_bounds__(BQ * 2, 2) void bwd_dq_kernel(BwdArgs a, BwdLists l
           dq[dg] = mfma32x32x16(columns_operand<D>(Ks, kg * 32 + 16 * c, dg, lane), ds[c], dq[dg]);
     }
   }
+  if (item.slot >= 0) {
+    store_part<D>(dq, a.parts + ((int64_t)item.slot * (BQ / 32) + wave) * (32 * D), lane);
+    return;
+  }
   barrier_tiles();  // the tiles are free
   store_rows_staged<D, __bf16>(dq, a.scale, (char*)tiles + wave * (32 * D * 2),
                                (__bf16*)a.dq + base + (int64_t)row0 * a.sn, a.sn, a.N - row0, lane);
 }
 
 // ---- dK and dV ----
+// The accumulators take 128 registers at d = 128 and the wavefront's K and V rows 64
+// more; with S and dP that is past the 256 that let two wavefronts share a SIMD, one's
+// exponentials beside the other's MFMAs.  So the V rows stay in LDS there, and to make
+// room the walked tiles have 32 rows.
+template <int D>
+constexpr bool kVInLds = D == 128;
+template <int D>
+constexpr int kWalkRows = kVInLds<D> ? 32 : 64;
+
 template <int BK, int D>
-__global__ __launch_bounds__(BK * 2, 1) void bwd_dkv_kernel(BwdArgs a, BwdLists lists) {
-  using T = Tile<BK, kWalk, D>;
-  __shared__ __attribute__((aligned(1024))) __bf16 tiles[2][2][kWalk * D];  // buffer, Q or dO
-  __shared__ __attribute__((aligned(1024))) float rows[2][2][kWalk];        // buffer, -lse or -D
+__global__ __launch_bounds__(BK * 2, 2) void bwd_dkv_kernel(BwdArgs a, BwdSide side) {
+  constexpr int W = kWalkRows<D>;
+  using T = Tile<BK, W, D>;
+  using TV = Tile<BK, BK, D>;
+  __shared__ __attribute__((aligned(1024))) __bf16 tiles[2][2][W * D];  // buffer, Q or dO
+  __shared__ __attribute__((aligned(1024))) __bf16 Vs[kVInLds<D> ? BK * D : 8];
+  __shared__ __attribute__((aligned(1024))) float rows[2][2][64];  // buffer, -lse or -D
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const Item item = item_of(a, lists, a.n_kb, a.n_qb);
+  const Item item = item_of(a, side, a.n_kb, a.n_qb);
+  if (item.cnt < 0) return;
   const int64_t base = (item.bh / a.H) * a.sb + (item.bh % a.H) * a.sh;
   const __bf16* Qb = (const __bf16*)a.q + base - kCopyShift;
   const __bf16* Gb = (const __bf16*)a.dout + base - kCopyShift;
-  const int shift = a.blk_q == 128 ? 1 : 0;
+  const int per = a.blk_q / W;  // tiles of a block: 1, 2 or 4
+  const int shift = per == 4 ? 2 : per - 1;
   auto block_at = [&](int i) { return min(max(item.list[i], 0), a.n_qb - 1); };
-  int n_tiles = item.cnt << shift;
-  if (shift && item.cnt > 0 && block_at(item.cnt - 1) * a.blk_q + kWalk >= a.N) --n_tiles;
-  auto row_of = [&](int t) { return block_at(t >> shift) * a.blk_q + (shift ? (t & 1) * kWalk : 0); };
+  int n_tiles = 0;
+  if (item.cnt > 0) {  // the last block of all may end early
+    const int left = min(a.blk_q, a.N - block_at(item.cnt - 1) * a.blk_q);
+    n_tiles = ((item.cnt - 1) << shift) + (left + W - 1) / W;
+  }
+  auto row_of = [&](int t) { return block_at(t >> shift) * a.blk_q + (t & (per - 1)) * W; };
   CopyPlan<T, D> cp;
   cp.init(wave, lane, a.sn);
   auto copy = [&](int t) {
     const int r0 = row_of(t);
-    issue_tile_copy<T, kWalk, D>(tiles[t & 1][0], Qb, r0, a.N, a.sn, wave, lane, cp);
-    issue_tile_copy<T, kWalk, D>(tiles[t & 1][1], Gb, r0, a.N, a.sn, wave, lane, cp);
-    if (wave < 2) {  // r0 + 63 < n_pad
+    issue_tile_copy<T, W, D>(tiles[t & 1][0], Qb, r0, a.N, a.sn, wave, lane, cp);
+    issue_tile_copy<T, W, D>(tiles[t & 1][1], Gb, r0, a.N, a.sn, wave, lane, cp);
+    if (wave < 2) {  // a lane a row, twice where there are 32; all below n_pad
       const float* from = (wave ? a.ndelta : a.nlse) + item.bh * a.n_pad + r0;
       const uint32_t to = __builtin_amdgcn_readfirstlane(
           (uint32_t)(uintptr_t)(SA_LDS void*)rows[t & 1][wave]);
-      asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(lane * 4), "s"(from), "{m0}"(to)
+      asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(lane % W * 4), "s"(from), "{m0}"(to)
                    : "memory");
     }
   };
+  if constexpr (kVInLds<D>) {
+    CopyPlan<TV, D> cv;
+    cv.init(wave, lane, a.sn);
+    if (n_tiles > 0)
+      issue_tile_copy<TV, BK, D>(Vs, (const __bf16*)a.v + base - kCopyShift, item.block * BK, a.N,
+                                 a.sn, wave, lane, cv);
+  }
   if (n_tiles > 0) copy(0);
 
   const int row0 = item.block * BK + wave * 32;
   const int krow = min(row0 + l32, a.N - 1);  // rows past N repeat the last: not stored
-  bf16x8 kf[D / 16], vf[D / 16];
+  bf16x8 kf[D / 16], vf[kVInLds<D> ? 1 : D / 16];
 #pragma unroll
   for (int dc = 0; dc < D / 16; ++dc) {
     const int64_t at = base + (int64_t)krow * a.sn + dc * 16 + half * 8;
     kf[dc] = *(const bf16x8*)((const __bf16*)a.k + at);
-    vf[dc] = *(const bf16x8*)((const __bf16*)a.v + at);
+    if constexpr (!kVInLds<D>) vf[dc] = *(const bf16x8*)((const __bf16*)a.v + at);
   }
+  auto v_operand = [&](int dc) {
+    if constexpr (!kVInLds<D>) return vf[dc];
+    const int r = wave * 32 + l32;
+    return lds_read_b128(Vs + r * D + (((2 * dc + half) ^ swz<D>(r)) << 3));
+  };
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int dg = 0; dg < D / 32; ++dg) dk[dg] = dv[dg] = f32x16{};
@@ -263,7 +491,7 @@ __global__ __launch_bounds__(BK * 2, 1) void bwd_dkv_kernel(BwdArgs a, BwdLists 
     barrier_tiles();
     if (t + 1 < n_tiles) copy(t + 1);
 #pragma unroll
-    for (int qg = 0; qg < kWalk / 32; ++qg) {
+    for (int qg = 0; qg < W / 32; ++qg) {
       f32x16 s, p;
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {  // register i holds row 16 (i / 8) + 8 half + i % 8
@@ -279,7 +507,7 @@ __global__ __launch_bounds__(BK * 2, 1) void bwd_dkv_kernel(BwdArgs a, BwdLists 
 #pragma unroll
       for (int dc = 0; dc < D / 16; ++dc) {
         s = mfma32x32x16(rows_operand<D>(Qs, qg * 32, dc, lane), kf[dc], s);
-        p = mfma32x32x16(rows_operand<D>(Gs, qg * 32, dc, lane), vf[dc], p);
+        p = mfma32x32x16(rows_operand<D>(Gs, qg * 32, dc, lane), v_operand(dc), p);
       }
       bf16x8 pf[2], ds[2];
 #pragma unroll
@@ -297,8 +525,15 @@ __global__ __launch_bounds__(BK * 2, 1) void bwd_dkv_kernel(BwdArgs a, BwdLists 
         }
     }
   }
+  if (item.slot >= 0) {
+    float* at = a.parts + ((int64_t)item.slot * (BK / 32) + wave) * (2 * 32 * D);
+    store_part<D>(dk, at, lane);
+    store_part<D>(dv, at + 32 * D, lane);
+    return;
+  }
   barrier_tiles();
   char* slice = (char*)tiles + wave * (32 * D * 2);
+  static_assert(sizeof(tiles) >= BK * D * 2, "the tiles hold the results");
   store_rows_staged<D, __bf16>(dk, a.scale, slice, (__bf16*)a.dk + base + (int64_t)row0 * a.sn, a.sn,
                                a.N - row0, lane);
   // the wavefront's own LDS reads and writes complete in order
@@ -306,40 +541,101 @@ __global__ __launch_bounds__(BK * 2, 1) void bwd_dkv_kernel(BwdArgs a, BwdLists 
                                a.N - row0, lane);
 }
 
+// Front entries of a table: parts at most, none where no list can be cut.
+int front_of(int64_t items, int n_walked, int least) {
+  if (n_walked <= least) return 0;
+  const int64_t most = items * ((n_walked + least - 1) / least);
+  return (int)(most < kFront ? (most + kXcds - 1) / kXcds * kXcds : kFront);
+}
+
+int64_t items_padded(int64_t items) { return (items + kXcds - 1) / kXcds * kXcds; }
+
 template <int D>
-hipError_t launch_d(const BwdArgs& a, const BwdLists& rows, const BwdLists& columns,
-                    hipStream_t stream) {
+hipError_t launch_d(const BwdArgs& a, const BwdWork& w, char* ws, hipStream_t stream) {
   const int64_t bh = (int64_t)a.B * a.H;
-  const unsigned dq_grid = (unsigned)(bh * a.n_qb), dkv_grid = (unsigned)(bh * a.n_kb);
-  const int R = 256 / (D / 8);
-  hipLaunchKernelGGL(bwd_rows_kernel<D>, dim3((unsigned)(bh * ((a.n_pad + R - 1) / R))), dim3(256), 0,
-                     stream, a);
+  const PrepGrid grid{(int)(((int64_t)a.mask_heads * a.n_qb + 3) / 4),
+                      (int)(((int64_t)a.mask_heads * a.n_kb + 3) / 4),
+                      (int)(bh * (a.n_pad / (256 / (D / 8))))};
+  hipLaunchKernelGGL(bwd_prep_kernel<D>,
+                     dim3((unsigned)(grid.row_blocks + grid.column_blocks + grid.token_blocks)),
+                     dim3(256), 0, stream, a, grid);
+  auto side = [&](const BwdSideWork& x, const int32_t* counts, int n_own) {
+    return PlanSide{counts, (int4*)(ws + x.table), (int4*)(ws + x.splits), (int32_t*)(ws + x.n_splits),
+                    n_own, x.front, (int)(bh * n_own), kLeast};
+  };
+  const PlanSide rows = side(w.rows, a.row_counts, a.n_qb);
+  const PlanSide columns = side(w.columns, a.column_counts, a.n_kb);
+  hipLaunchKernelGGL(bwd_plan_kernel, dim3(kXcds + 1, 2), dim3(1024), 0, stream, rows, columns,
+                     a.mask_heads, (int)bh);
+  const BwdSide r{a.row_lists, rows.table, rows.splits, rows.n_splits};
+  const BwdSide c{a.column_lists, columns.table, columns.splits, columns.n_splits};
+  const unsigned dq_grid = (unsigned)(rows.front + items_padded(rows.n_items));
+  const unsigned dkv_grid = (unsigned)(columns.front + items_padded(columns.n_items));
   if (a.blk_q == 128)
-    hipLaunchKernelGGL((bwd_dq_kernel<128, D>), dim3(dq_grid), dim3(256), 0, stream, a, rows);
+    hipLaunchKernelGGL((bwd_dq_kernel<128, D>), dim3(dq_grid), dim3(256), 0, stream, a, r);
   else
-    hipLaunchKernelGGL((bwd_dq_kernel<64, D>), dim3(dq_grid), dim3(128), 0, stream, a, rows);
+    hipLaunchKernelGGL((bwd_dq_kernel<64, D>), dim3(dq_grid), dim3(128), 0, stream, a, r);
+  auto join = [&](const BwdSide& x, const PlanSide& p, int blk, int results) {
+    if (p.front == 0) return;
+    const int64_t waves = (int64_t)(p.front / 2) * (blk / 32) * (D / 32) * results;
+    hipLaunchKernelGGL(bwd_join_kernel<D>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, a, x,
+                       p.n_own, blk, results);
+  };
+  join(r, rows, a.blk_q, 1);
   if (a.blk_k == 128)
-    hipLaunchKernelGGL((bwd_dkv_kernel<128, D>), dim3(dkv_grid), dim3(256), 0, stream, a, columns);
+    hipLaunchKernelGGL((bwd_dkv_kernel<128, D>), dim3(dkv_grid), dim3(256), 0, stream, a, c);
   else
-    hipLaunchKernelGGL((bwd_dkv_kernel<64, D>), dim3(dkv_grid), dim3(128), 0, stream, a, columns);
+    hipLaunchKernelGGL((bwd_dkv_kernel<64, D>), dim3(dkv_grid), dim3(128), 0, stream, a, c);
+  join(c, columns, a.blk_k, 2);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_column_lists(const uint64_t* mask_bits, int H, int n_qb, int n_kb, int32_t* counts,
-                               int32_t* lists, hipStream_t stream) {
-  const int64_t columns = (int64_t)H * n_kb;
-  hipLaunchKernelGGL(column_lists_kernel, dim3((unsigned)((columns + 3) / 4)), dim3(256), 0, stream,
-                     mask_bits, columns, n_qb, n_kb, counts, lists);
-  return hipGetLastError();
+BwdWork bwd_work(int B, int H, int mask_heads, int n_qb, int n_kb, int n_pad, int d, int blk_q,
+                 int blk_k) {
+  BwdWork w;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t from = at;
+    at += (bytes + 255) / 256 * 256;
+    return from;
+  };
+  const int64_t bh = (int64_t)B * H;
+  auto side = [&](int n_own, int n_walked) {
+    BwdSideWork x;
+    x.front = front_of(bh * n_own, n_walked, kLeast);
+    x.counts = take((size_t)mask_heads * n_own * 4);
+    x.lists = take((size_t)mask_heads * n_own * n_walked * 4);
+    x.table = take((size_t)(x.front + items_padded(bh * n_own)) * sizeof(int4));
+    x.splits = take((size_t)(x.front / 2) * sizeof(int4));
+    x.n_splits = take(4);
+    return x;
+  };
+  w.rows = side(n_qb, n_kb);
+  w.columns = side(n_kb, n_qb);
+  w.nlse = take((size_t)bh * n_pad * 4);
+  w.ndelta = take((size_t)bh * n_pad * 4);
+  // the two kernels' parts take turns
+  const size_t dq = (size_t)w.rows.front * blk_q * d * 4, dkv = (size_t)w.columns.front * blk_k * d * 8;
+  w.parts = take(dq > dkv ? dq : dkv);
+  w.total = at;
+  return w;
 }
 
-hipError_t launch_attention_bwd(const BwdArgs& a, const BwdLists& rows, const BwdLists& columns,
-                                hipStream_t stream) {
+hipError_t launch_attention_bwd(const BwdArgs& a, void* workspace, hipStream_t stream) {
+  char* ws = (char*)workspace;
+  const BwdWork w = bwd_work(a.B, a.H, a.mask_heads, a.n_qb, a.n_kb, a.n_pad, a.d, a.blk_q, a.blk_k);
   BwdArgs b = a;
   b.c_log2 = a.scale * kLog2e;
-  return a.d == 128 ? launch_d<128>(b, rows, columns, stream) : launch_d<64>(b, rows, columns, stream);
+  b.row_counts = (int32_t*)(ws + w.rows.counts);
+  b.row_lists = (int32_t*)(ws + w.rows.lists);
+  b.column_counts = (int32_t*)(ws + w.columns.counts);
+  b.column_lists = (int32_t*)(ws + w.columns.lists);
+  b.nlse = (float*)(ws + w.nlse);
+  b.ndelta = (float*)(ws + w.ndelta);
+  b.parts = (float*)(ws + w.parts);
+  return a.d == 128 ? launch_d<128>(b, w, ws, stream) : launch_d<64>(b, w, ws, stream);
 }
 
 }  // namespace sa

@@ -100,13 +100,6 @@ int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk);
 
 hipError_t launch_selected_decode(const DecodeArgs& a, hipStream_t stream);
 
-// Lists that a kernel walks and the order of its items.
-struct BwdLists {
-  const int32_t* counts;
-  const int32_t* lists;
-  const int32_t* order;
-};
-
 struct BwdArgs {
   const void* q;
   const void* k;
@@ -114,24 +107,50 @@ struct BwdArgs {
   const void* out;
   const void* dout;
   const float* lse;
+  const uint64_t* mask;
   void* dq;
   void* dk;
   void* dv;
-  float* nlse;    // float [B H][n_pad], n_pad = N rounded up to 128
-  float* ndelta;  // the same
-  int B, H, N, d, blk_q, blk_k, n_qb, n_kb, n_pad;
+  int B, H, N, d, blk_q, blk_k, n_qb, n_kb;
+  int n_pad;       // N rounded up to 128
   int mask_heads;  // H, or B H with a mask for every batch entry
   float scale;
   int64_t sb, sh;  // element strides: batch, head, token
   int sn;
-  float c_log2;  // set by the launcher
+  // set by the launcher: the exponent's factor, and the workspace
+  float c_log2;
+  int32_t* row_counts;     // [mask_heads][n_qb]
+  int32_t* row_lists;      // [mask_heads][n_qb][n_kb]
+  int32_t* column_counts;  // [mask_heads][n_kb]
+  int32_t* column_lists;   // [mask_heads][n_kb][n_qb]
+  float* nlse;             // [B H][n_pad]
+  float* ndelta;
+  float* parts;
 };
 
-hipError_t launch_column_lists(const uint64_t* mask_bits, int H, int n_qb, int n_kb, int32_t* counts,
-                               int32_t* lists, hipStream_t stream);
+// Lists that a kernel walks, and the plan of its workgroups.
+struct BwdSide {
+  const int32_t* lists;
+  const int4* table;
+  const int4* splits;
+  const int32_t* n_splits;
+};
 
-hipError_t launch_attention_bwd(const BwdArgs& a, const BwdLists& rows, const BwdLists& columns,
-                                hipStream_t stream);
+// Offsets in the workspace; `front`: entries of a table for parts of cut lists.
+struct BwdSideWork {
+  size_t counts, lists, table, splits, n_splits;
+  int front;
+};
+
+struct BwdWork {
+  BwdSideWork rows, columns;
+  size_t nlse, ndelta, parts, total;
+};
+
+BwdWork bwd_work(int B, int H, int mask_heads, int n_qb, int n_kb, int n_pad, int d, int blk_q,
+                 int blk_k);
+
+hipError_t launch_attention_bwd(const BwdArgs& a, void* workspace, hipStream_t stream);
 
 hipError_t launch_prepass(const uint64_t* mask_bits, int H, int n_qb, int n_kb, int32_t* counts,
                           int32_t* lists, hipStream_t stream);

@@ -150,25 +150,6 @@ int attn_shape(int B, int H, int N, int d, int blk_q, int blk_k) {
   return SA_OK;
 }
 
-// Workspace of sa_bsattn_bwd: lists by rows and by columns, and two floats a row.
-struct BwdWs {
-  size_t counts, lists, order, ccounts, clists, corder, nlse, ndelta, total;
-};
-
-BwdWs bwd_ws(int64_t B, int64_t H, int64_t mask_heads, int64_t n_qb, int64_t n_kb, int64_t n_pad) {
-  BwdWs w;
-  w.counts = 0;
-  w.lists = w.counts + align_up((size_t)(mask_heads * n_qb) * 4);
-  w.order = w.lists + align_up((size_t)(mask_heads * n_qb * n_kb) * 4);
-  w.ccounts = w.order + align_up((size_t)(B * H * n_qb) * 4);
-  w.clists = w.ccounts + align_up((size_t)(mask_heads * n_kb) * 4);
-  w.corder = w.clists + align_up((size_t)(mask_heads * n_qb * n_kb) * 4);
-  w.nlse = w.corder + align_up((size_t)(B * H * n_kb) * 4);
-  w.ndelta = w.nlse + align_up((size_t)(B * H * n_pad) * 4);
-  w.total = w.ndelta + align_up((size_t)(B * H * n_pad) * 4);
-  return w;
-}
-
 int decode_shape(int B, int Hq, int Hkv, int cap, int d, int blk, int topk) {
   if (B < 1 || Hq < 1 || Hkv < 1 || cap < 1 || topk < 1 || Hq % Hkv) return SA_ERR_INVALID_ARG;
   if ((d != 64 && d != 128) || !blk_ok(blk)) return SA_ERR_UNSUPPORTED;
@@ -333,7 +314,9 @@ SA_API int sa_selected_attn_fwd(const void* q, const void* k, const void* v,
 SA_API size_t sa_bsattn_bwd_workspace(int B, int H, int N, int d, int blk_q, int blk_k,
                                       int mask_batches) {
   if (attn_shape(B, H, N, d, blk_q, blk_k) != SA_OK || (mask_batches != 1 && mask_batches != B)) return 0;
-  return bwd_ws(B, H, (int64_t)mask_batches * H, cdiv(N, blk_q), cdiv(N, blk_k), cdiv(N, 128) * 128).total;
+  if ((int64_t)mask_batches * H * cdiv(N, blk_q) > kMaxGrid / cdiv(N, blk_k)) return 0;
+  return sa::bwd_work(B, H, mask_batches * H, (int)cdiv(N, blk_q), (int)cdiv(N, blk_k),
+                      (int)(cdiv(N, 128) * 128), d, blk_q, blk_k).total;
 }
 
 SA_API int sa_bsattn_bwd(const void* dout, const void* q, const void* k, const void* v,
@@ -357,32 +340,41 @@ SA_API int sa_bsattn_bwd(const void* dout, const void* q, const void* k, const v
   const int n_qb = (int)cdiv(N, blk_q), n_kb = (int)cdiv(N, blk_k);
   const int n_pad = (int)(cdiv(N, 128) * 128);
   const int mask_heads = mask_batches * H;
-  const BwdWs w = bwd_ws(B, H, mask_heads, n_qb, n_kb, n_pad);
+  if ((int64_t)mask_heads * n_qb > kMaxGrid / n_kb) return SA_ERR_UNSUPPORTED;
+  const size_t ws_bytes = sa::bwd_work(B, H, mask_heads, n_qb, n_kb, n_pad, d, blk_q, blk_k).total;
   const size_t bytes = (size_t)B * H * N * d * 2;
   const Span ins[7] = {{dout, bytes}, {q, bytes}, {k, bytes}, {v, bytes}, {out, bytes},
                        {lse, (size_t)B * H * N * 4},
                        {mask_bits, (size_t)mask_heads * n_qb * cdiv(n_kb, 64) * 8}};
-  const Span outs[4] = {{dq, bytes}, {dk, bytes}, {dv, bytes}, {workspace, w.total}};
+  const Span outs[4] = {{dq, bytes}, {dk, bytes}, {dv, bytes}, {workspace, ws_bytes}};
   if (clash(outs, ins)) return SA_ERR_INVALID_ARG;
 
-  hipStream_t s = (hipStream_t)stream;
-  char* ws = (char*)workspace;
-  auto ints = [&](size_t off) { return (int32_t*)(ws + off); };
-  const int groups = mask_batches == 1 ? B : 1;  // batch entries that share each mask row
-  hipError_t e = sa::launch_prepass(mask_bits, mask_heads, n_qb, n_kb, ints(w.counts), ints(w.lists), s);
-  if (e == hipSuccess)
-    e = sa::launch_column_lists(mask_bits, mask_heads, n_qb, n_kb, ints(w.ccounts), ints(w.clists), s);
-  if (e == hipSuccess) e = sa::launch_schedule(ints(w.counts), groups, mask_heads, n_qb, ints(w.order), s);
-  if (e == hipSuccess)
-    e = sa::launch_schedule(ints(w.ccounts), groups, mask_heads, n_kb, ints(w.corder), s);
-  if (e == hipSuccess) {
-    sa::BwdArgs a{q, k, v, out, dout, lse, dq, dk, dv, (float*)(ws + w.nlse), (float*)(ws + w.ndelta),
-                  B, H, N, d, blk_q, blk_k, n_qb, n_kb, n_pad, mask_heads, scale,
-                  (int64_t)H * N * d, bnhd ? (int64_t)d : (int64_t)N * d, bnhd ? H * d : d, 0.f};
-    e = sa::launch_attention_bwd(a, {ints(w.counts), ints(w.lists), ints(w.order)},
-                                 {ints(w.ccounts), ints(w.clists), ints(w.corder)}, s);
-  }
-  return status(e);
+  sa::BwdArgs a{};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.out = out;
+  a.dout = dout;
+  a.lse = lse;
+  a.mask = mask_bits;
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  a.B = B;
+  a.H = H;
+  a.N = N;
+  a.d = d;
+  a.blk_q = blk_q;
+  a.blk_k = blk_k;
+  a.n_qb = n_qb;
+  a.n_kb = n_kb;
+  a.n_pad = n_pad;
+  a.mask_heads = mask_heads;
+  a.scale = scale;
+  a.sb = (int64_t)H * N * d;
+  a.sh = bnhd ? d : (int64_t)N * d;
+  a.sn = bnhd ? H * d : d;
+  return status(sa::launch_attention_bwd(a, workspace, (hipStream_t)stream));
 }
 
 SA_API size_t sa_selected_decode_workspace(int B, int Hq, int Hkv, int cap, int d, int blk, int topk) {
