@@ -6,6 +6,7 @@ fallback: if the library cannot be loaded the functions raise.
 """
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -480,7 +481,8 @@ class Plan:
 # ------------------------------------------------- around the attention ---
 #
 # Tensors may be on any GPU, all on the same one; the work goes to that GPU's
-# current stream, or to ``stream``, which has to be of that GPU.
+# current stream, or to ``stream``, which has to be of that GPU.  The checks are
+# written for small calls, which take the host longer than the GPU.
 
 _PAIRS = {"interleaved": SA_PAIRS_INTERLEAVED, "halves": SA_PAIRS_HALVES}
 _LAYOUTS = {"bhnd": SA_LAYOUT_BHND, "bnhd": SA_LAYOUT_BNHD}
@@ -491,49 +493,66 @@ def _named(table, key, name):
     return table[key]
 
 
-def _tensors(**named):
-    """Type and device checks of the arguments; None stands for one that is left out."""
-    torch = _torch()
-    device = None
-    for name, t in named.items():
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor):
-            raise TypeError("%s must be a torch tensor" % name)
-        if t.device.type != "cuda":
-            raise ValueError("%s must be on the GPU, got %s" % (name, t.device))
-        device = t.device if device is None else device
-        _need(t.device == device, "%s is on %s, others are on %s" % (name, t.device, device))
-    return device
+def _device(t, name):
+    """Index of the GPU that the call's first tensor is on."""
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError("%s must be a torch tensor" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU, got %s" % (name, t.device))
+    return t.get_device()
 
 
-def _on(device, stream):
-    """The device made current for the call, whose stream has to be of it."""
-    torch = _torch()
-    _need(stream is None or stream.device == device, "stream is not of device %s" % (device,))
-    return torch.cuda.device(device)
+def _ptr(t, dtype, name, dev):
+    """Address of a contiguous tensor on GPU ``dev``."""
+    if not (isinstance(t, _torch().Tensor) and t.dtype == dtype and t.is_contiguous()):
+        _dev_ptr(t, dtype, name)  # raises
+    if t.get_device() != dev:
+        _need(_device(t, name) == dev, "%s is on GPU %d, others are on GPU %d"
+              % (name, t.get_device(), dev))
+    return t.data_ptr()
 
 
-def _rows_ptr(t, name):
-    """Pointer and strides of bf16 rows whose last dimension is contiguous; the strides of the
+@functools.lru_cache(maxsize=256)
+def _strides(*s):
+    return (ctypes.c_int64 * 3)(*s)
+
+
+def _rows_ptr(t, name, dev):
+    """Address and strides of bf16 rows whose last dimension is contiguous; the strides of the
     others (any order, 0 for a repeated row) in the tensor's order."""
     torch = _torch()
+    if _device(t, name) != dev:
+        raise ValueError("%s is on GPU %d, others are on GPU %d" % (name, t.get_device(), dev))
     if t.dtype != torch.bfloat16:
         raise TypeError("%s must be %s, got %s" % (name, torch.bfloat16, t.dtype))
-    _need(t.stride(-1) == 1 or t.shape[-1] == 1, "%s must be contiguous in its last dimension" % name)
+    (n0, n1, n2, n3), (s0, s1, s2, s3) = t.shape, t.stride()
+    _need(s3 == 1 or n3 == 1, "%s must be contiguous in its last dimension" % name)
     # the stride of a dimension of one entry means nothing
-    strides = [s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape[:-1])]
-    _need(all(s % 8 == 0 for s in strides) and t.data_ptr() % 16 == 0,
-          "%s: rows must be 16-byte aligned (strides %s)" % (name, tuple(t.stride())))
-    return ctypes.c_void_p(t.data_ptr()), (ctypes.c_int64 * 3)(*strides)
+    s0, s1, s2 = s0 if n0 > 1 else 0, s1 if n1 > 1 else 0, s2 if n2 > 1 else 0
+    ptr = t.data_ptr()
+    _need((s0 | s1 | s2) % 8 == 0 and ptr % 16 == 0,
+          "%s: rows must be 16-byte aligned" % name)
+    return ptr, _strides(s0, s1, s2)
 
 
-def _opt_ptr(t, dtype, name):
-    return None if t is None else _dev_ptr(t, dtype, name)
+def _run(fn, dev, stream, args, made):
+    """Calls ``fn`` with GPU ``dev`` current, on its current stream or ``stream``; ``made`` are the
+    tensors allocated for the call."""
+    torch = _torch()
+    if stream is None and torch.cuda.current_device() == dev:
+        st = getattr(load(), fn)(*args, torch.cuda.current_stream().cuda_stream)
+    else:
+        _need(stream is None or stream.device_index == dev, "stream is not of GPU %d" % dev)
+        with torch.cuda.device(dev):
+            st = getattr(load(), fn)(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+            _used_on(stream, *made)
+    if st != SA_OK:
+        raise SAError(fn, st)
 
 
-def _workspace(lib, fn, device, *sizes):
-    return _torch().empty(max(1, getattr(lib, fn)(*sizes)), dtype=_torch().uint8, device=device)
+def _workspace(like, fn, *sizes):
+    torch = _torch()
+    return like.new_empty(max(1, getattr(load(), fn)(*sizes)), dtype=torch.uint8)
 
 
 def _mask_arg(m, B, H, n_qb, n_kb, name):
@@ -541,6 +560,8 @@ def _mask_arg(m, B, H, n_qb, n_kb, name):
     torch = _torch()
     if m is None:
         return None, 1
+    if not isinstance(m, torch.Tensor):
+        raise TypeError("%s must be a torch tensor" % name)
     if m.dtype == torch.uint64:
         m = m.view(torch.int64)
     shape = (H, n_qb, (n_kb + 63) // 64)
@@ -553,15 +574,17 @@ def _mask_arg(m, B, H, n_qb, n_kb, name):
 def _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs, layout):
     _need(q.dim() == 4 and k.dim() == 4, "q and k must be [B, N, heads, d]")
     B, N, Hq, d = q.shape
-    Hk = k.shape[2]
-    _need(tuple(k.shape) == (B, N, Hk, d), "k has shape %s, expected [%d, %d, heads, %d]"
+    B2, N2, Hk, d2 = k.shape
+    _need(B2 == B and N2 == N and d2 == d, "k has shape %s, expected [%d, %d, heads, %d]"
           % (tuple(k.shape), B, N, d))
-    _need(tuple(wq.shape) == (d,) and tuple(wk.shape) == (d,), "wq and wk must be [d]")
+    _need(wq.shape == (d,) and wk.shape == (d,), "wq and wk must be [d]")
     _need(cos.dim() == 2 and cos.shape == sin.shape, "cos and sin must be [positions, rot / 2]")
-    _need(positions is None or tuple(positions.shape) == (B, N), "positions must be [B, N]")
-    _need(positions is not None or cos.shape[0] >= N, "cos and sin have %d positions for %d tokens"
-          % (cos.shape[0], N))
-    return (B, N, Hq, Hk, d, 2 * cos.shape[1], cos.shape[0], _named(_PAIRS, pairs, "pairs"),
+    n_pos, half = cos.shape
+    if positions is None:
+        _need(n_pos >= N, "cos and sin have %d positions for %d tokens" % (n_pos, N))
+    else:
+        _need(positions.shape == (B, N), "positions must be [B, N]")
+    return (B, N, Hq, Hk, d, 2 * half, n_pos, _named(_PAIRS, pairs, "pairs"),
             _named(_LAYOUTS, layout, "layout"))
 
 
@@ -579,21 +602,20 @@ def qk_norm_rope(q, k, wq, wk, cos, sin, positions=None, eps=1e-6, pairs="interl
     (``layout`` "bhnd", as the attention reads them) or [B, N, H, d] ("bnhd").
     """
     torch = _torch()
-    device = _tensors(q=q, k=k, wq=wq, wk=wk, cos=cos, sin=sin, positions=positions)
+    f32 = torch.float32
+    dev = _device(q, "q")
+    q_ptr, q_str = _rows_ptr(q, "q", dev)
+    k_ptr, k_str = _rows_ptr(k, "k", dev)
+    ptrs = (_ptr(wq, f32, "wq", dev), _ptr(wk, f32, "wk", dev), _ptr(cos, f32, "cos", dev),
+            _ptr(sin, f32, "sin", dev),
+            None if positions is None else _ptr(positions, torch.int32, "positions", dev))
     B, N, Hq, Hk, d, rot, n_pos, pr, lay = _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs,
                                                         layout)
-    lib = load()
-    with _on(device, stream):
-        q_out, k_out = (torch.empty(_heads_shape(lay, B, N, H, d), dtype=torch.bfloat16,
-                                    device=device) for H in (Hq, Hk))
-        st = lib.sa_qk_norm_rope(
-            *_rows_ptr(q, "q"), *_rows_ptr(k, "k"), _dev_ptr(wq, torch.float32, "wq"),
-            _dev_ptr(wk, torch.float32, "wk"), _dev_ptr(cos, torch.float32, "cos"),
-            _dev_ptr(sin, torch.float32, "sin"), _opt_ptr(positions, torch.int32, "positions"),
-            _dev_ptr(q_out, torch.bfloat16, "q_out"), _dev_ptr(k_out, torch.bfloat16, "k_out"),
-            B, N, Hq, Hk, d, rot, n_pos, float(eps), pr, lay, _stream(stream))
-        _check("sa_qk_norm_rope", st)
-        _used_on(stream, q_out, k_out)
+    q_out = q.new_empty(_heads_shape(lay, B, N, Hq, d))
+    k_out = q.new_empty(_heads_shape(lay, B, N, Hk, d))
+    _run("sa_qk_norm_rope", dev, stream,
+         (q_ptr, q_str, k_ptr, k_str, *ptrs, q_out.data_ptr(), k_out.data_ptr(), B, N, Hq, Hk, d, rot,
+          n_pos, eps, pr, lay), (q_out, k_out))
     return q_out, k_out
 
 
@@ -605,29 +627,26 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, wq, wk, cos, sin, positions=None, eps
     (dq bf16 [B, N, Hq, d], dk bf16 [B, N, Hk, d], dwq float32 [d], dwk float32 [d]).
     """
     torch = _torch()
-    device = _tensors(dq_out=dq_out, dk_out=dk_out, q=q, k=k, wq=wq, wk=wk, cos=cos, sin=sin,
-                      positions=positions)
+    f32, b16 = torch.float32, torch.bfloat16
+    dev = _device(q, "q")
+    q_ptr, q_str = _rows_ptr(q, "q", dev)
+    k_ptr, k_str = _rows_ptr(k, "k", dev)
+    grads = _ptr(dq_out, b16, "dq_out", dev), _ptr(dk_out, b16, "dk_out", dev)
+    ptrs = (_ptr(wq, f32, "wq", dev), _ptr(wk, f32, "wk", dev), _ptr(cos, f32, "cos", dev),
+            _ptr(sin, f32, "sin", dev),
+            None if positions is None else _ptr(positions, torch.int32, "positions", dev))
     B, N, Hq, Hk, d, rot, n_pos, pr, lay = _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs,
                                                         layout)
     for t, H, name in ((dq_out, Hq, "dq_out"), (dk_out, Hk, "dk_out")):
-        _need(tuple(t.shape) == _heads_shape(lay, B, N, H, d), "%s has shape %s, expected %s"
+        _need(t.shape == _heads_shape(lay, B, N, H, d), "%s has shape %s, expected %s"
               % (name, tuple(t.shape), _heads_shape(lay, B, N, H, d)))
-    lib = load()
-    with _on(device, stream):
-        dq, dk = (torch.empty((B, N, H, d), dtype=torch.bfloat16, device=device) for H in (Hq, Hk))
-        dwq, dwk = (torch.empty(d, dtype=torch.float32, device=device) for _ in range(2))
-        ws = _workspace(lib, "sa_qk_norm_rope_bwd_workspace", device, d)
-        st = lib.sa_qk_norm_rope_bwd(
-            _dev_ptr(dq_out, torch.bfloat16, "dq_out"), _dev_ptr(dk_out, torch.bfloat16, "dk_out"),
-            *_rows_ptr(q, "q"), *_rows_ptr(k, "k"), _dev_ptr(wq, torch.float32, "wq"),
-            _dev_ptr(wk, torch.float32, "wk"), _dev_ptr(cos, torch.float32, "cos"),
-            _dev_ptr(sin, torch.float32, "sin"), _opt_ptr(positions, torch.int32, "positions"),
-            _dev_ptr(dq, torch.bfloat16, "dq"), _dev_ptr(dk, torch.bfloat16, "dk"),
-            _dev_ptr(dwq, torch.float32, "dwq"), _dev_ptr(dwk, torch.float32, "dwk"),
-            _dev_ptr(ws, torch.uint8, "workspace"), B, N, Hq, Hk, d, rot, n_pos, float(eps), pr,
-            lay, _stream(stream))
-        _check("sa_qk_norm_rope_bwd", st)
-        _used_on(stream, dq, dk, dwq, dwk, ws)
+    dq, dk = q.new_empty((B, N, Hq, d)), q.new_empty((B, N, Hk, d))
+    dwq, dwk = wq.new_empty(d), wq.new_empty(d)
+    ws = _workspace(q, "sa_qk_norm_rope_bwd_workspace", d)
+    _run("sa_qk_norm_rope_bwd", dev, stream,
+         (*grads, q_ptr, q_str, k_ptr, k_str, *ptrs, dq.data_ptr(), dk.data_ptr(), dwq.data_ptr(),
+          dwk.data_ptr(), ws.data_ptr(), B, N, Hq, Hk, d, rot, n_pos, eps, pr, lay),
+         (dq, dk, dwq, dwk, ws))
     return dq, dk, dwq, dwk
 
 
@@ -637,18 +656,13 @@ def block_means(x, blk, stream=None):
     x: bf16 [B, H, N, d], the first three dimensions of any strides (a transposed
     [B, N, H, d], or the tokens of a cache's newly finished block).
     """
-    torch = _torch()
-    device = _tensors(x=x)
+    dev = _device(x, "x")
     _need(x.dim() == 4, "x must be [B, H, N, d]")
+    ptr, strides = _rows_ptr(x, "x", dev)
     B, H, N, d = x.shape
     _need(blk in (64, 128), "blk must be 64 or 128, got %r" % (blk,))
-    lib = load()
-    with _on(device, stream):
-        means = torch.empty((B, H, -(-N // blk), d), dtype=torch.float32, device=device)
-        st = lib.sa_block_means(*_rows_ptr(x, "x"), _dev_ptr(means, torch.float32, "means"), B, H, N,
-                                d, int(blk), _stream(stream))
-        _check("sa_block_means", st)
-        _used_on(stream, means)
+    means = x.new_empty((B, H, -(-N // blk), d), dtype=_torch().float32)
+    _run("sa_block_means", dev, stream, (ptr, strides, means.data_ptr(), B, H, N, d, blk), (means,))
     return means
 
 
@@ -660,24 +674,21 @@ def block_select(q_means, k_means, topk, candidates=None, keep=None, stream=None
     them.  Each int64 [H, n_qb, W], shared by the batch, or [B, H, n_qb, W].
     """
     torch = _torch()
-    device = _tensors(q_means=q_means, k_means=k_means, candidates=candidates, keep=keep)
+    dev = _device(q_means, "q_means")
+    q_ptr = _ptr(q_means, torch.float32, "q_means", dev)
+    k_ptr = _ptr(k_means, torch.float32, "k_means", dev)
     _need(q_means.dim() == 4 and k_means.dim() == 4, "q_means and k_means must be [B, H, blocks, d]")
     B, H, n_qb, d = q_means.shape
-    n_kb = k_means.shape[2]
-    _need(tuple(k_means.shape) == (B, H, n_kb, d), "k_means has shape %s, expected [%d, %d, blocks, %d]"
+    B2, H2, n_kb, d2 = k_means.shape
+    _need(B2 == B and H2 == H and d2 == d, "k_means has shape %s, expected [%d, %d, blocks, %d]"
           % (tuple(k_means.shape), B, H, d))
     candidates, cb = _mask_arg(candidates, B, H, n_qb, n_kb, "candidates")
     keep, kb = _mask_arg(keep, B, H, n_qb, n_kb, "keep")
-    lib = load()
-    with _on(device, stream):
-        mask = torch.empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64, device=device)
-        st = lib.sa_block_select(
-            _dev_ptr(q_means, torch.float32, "q_means"), _dev_ptr(k_means, torch.float32, "k_means"),
-            _opt_ptr(candidates, torch.int64, "candidates"), cb, _opt_ptr(keep, torch.int64, "keep"),
-            kb, _dev_ptr(mask, torch.int64, "mask_bits"), None, None, B, H, n_qb, n_kb, d, int(topk),
-            _stream(stream))
-        _check("sa_block_select", st)
-        _used_on(stream, mask)
+    mask = q_means.new_empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64)
+    _run("sa_block_select", dev, stream,
+         (q_ptr, k_ptr, None if candidates is None else _ptr(candidates, torch.int64, "candidates", dev),
+          cb, None if keep is None else _ptr(keep, torch.int64, "keep", dev), kb, mask.data_ptr(), None,
+          None, B, H, n_qb, n_kb, d, int(topk)), (mask,))
     return mask
 
 
@@ -690,7 +701,9 @@ def selected_attn_fwd(q, k, v, blk_q, blk_k, topk, candidates=None, keep=None, s
     the mask is what ``bsattn_bwd`` takes.
     """
     torch = _torch()
-    device = _tensors(q=q, k=k, v=v, candidates=candidates, keep=keep)
+    b16 = torch.bfloat16
+    dev = _device(q, "q")
+    ptrs = _ptr(q, b16, "q", dev), _ptr(k, b16, "k", dev), _ptr(v, b16, "v", dev)
     _need(q.dim() == 4, "q must be [B, H, N, d]")
     B, H, N, d = q.shape
     _same_shape(q, (k, v), ("k", "v"))
@@ -700,21 +713,15 @@ def selected_attn_fwd(q, k, v, blk_q, blk_k, topk, candidates=None, keep=None, s
     keep, kb = _mask_arg(keep, B, H, n_qb, n_kb, "keep")
     if scale is None:
         scale = 1.0 / float(d) ** 0.5
-    lib = load()
-    with _on(device, stream):
-        out = torch.empty_like(q)
-        lse = torch.empty((B, H, N), dtype=torch.float32, device=device)
-        mask = torch.empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64, device=device)
-        ws = _workspace(lib, "sa_selected_attn_workspace", device, B, H, N, d, blk_q, blk_k)
-        st = lib.sa_selected_attn_fwd(
-            _dev_ptr(q, torch.bfloat16, "q"), _dev_ptr(k, torch.bfloat16, "k"),
-            _dev_ptr(v, torch.bfloat16, "v"), _opt_ptr(candidates, torch.int64, "candidates"), cb,
-            _opt_ptr(keep, torch.int64, "keep"), kb, _dev_ptr(out, torch.bfloat16, "out"),
-            _dev_ptr(lse, torch.float32, "lse"), _dev_ptr(mask, torch.int64, "mask_bits"),
-            _dev_ptr(ws, torch.uint8, "workspace"), B, H, N, d, int(blk_q), int(blk_k), int(topk),
-            float(scale), _stream(stream))
-        _check("sa_selected_attn_fwd", st)
-        _used_on(stream, out, lse, mask, ws)
+    out = q.new_empty((B, H, N, d))
+    lse = q.new_empty((B, H, N), dtype=torch.float32)
+    mask = q.new_empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64)
+    ws = _workspace(q, "sa_selected_attn_workspace", B, H, N, d, blk_q, blk_k)
+    _run("sa_selected_attn_fwd", dev, stream,
+         (*ptrs, None if candidates is None else _ptr(candidates, torch.int64, "candidates", dev), cb,
+          None if keep is None else _ptr(keep, torch.int64, "keep", dev), kb, out.data_ptr(),
+          lse.data_ptr(), mask.data_ptr(), ws.data_ptr(), B, H, N, d, blk_q, blk_k, int(topk), scale),
+         (out, lse, mask, ws))
     return out, lse, mask
 
 
@@ -728,9 +735,10 @@ def bsattn_bwd(dout, q, k, v, out, lse, mask_bits, blk_q, blk_k, scale=None, lay
     ``selected_attn_fwd`` returns them.
     """
     torch = _torch()
-    if not isinstance(mask_bits, torch.Tensor):
-        mask_bits = mask_to_device(mask_bits, q.device)
-    device = _tensors(dout=dout, q=q, k=k, v=v, out=out, lse=lse, mask_bits=mask_bits)
+    b16 = torch.bfloat16
+    dev = _device(q, "q")
+    ptrs = (_ptr(dout, b16, "dout", dev), _ptr(q, b16, "q", dev), _ptr(k, b16, "k", dev),
+            _ptr(v, b16, "v", dev), _ptr(out, b16, "out", dev), _ptr(lse, torch.float32, "lse", dev))
     lay = _named(_LAYOUTS, layout, "layout")
     _need(q.dim() == 4, "q must have four dimensions")
     if lay == SA_LAYOUT_BHND:
@@ -738,25 +746,18 @@ def bsattn_bwd(dout, q, k, v, out, lse, mask_bits, blk_q, blk_k, scale=None, lay
     else:
         B, N, H, d = q.shape
     _same_shape(q, (dout, k, v, out), ("dout", "k", "v", "out"))
-    _need(tuple(lse.shape) == (B, H, N), "lse must have shape %s" % ((B, H, N),))
+    _need(lse.shape == (B, H, N), "lse must have shape %s" % ((B, H, N),))
     _need(blk_q in (64, 128) and blk_k in (64, 128), "blk_q and blk_k must be 64 or 128")
+    if not isinstance(mask_bits, torch.Tensor):
+        mask_bits = mask_to_device(mask_bits, q.device)
     m, batches = _mask_arg(mask_bits, B, H, -(-N // blk_q), -(-N // blk_k), "mask_bits")
     if scale is None:
         scale = 1.0 / float(d) ** 0.5
-    lib = load()
-    with _on(device, stream):
-        dq, dk, dv = (torch.empty_like(q) for _ in range(3))
-        ws = _workspace(lib, "sa_bsattn_bwd_workspace", device, B, H, N, d, blk_q, blk_k, batches)
-        st = lib.sa_bsattn_bwd(
-            _dev_ptr(dout, torch.bfloat16, "dout"), _dev_ptr(q, torch.bfloat16, "q"),
-            _dev_ptr(k, torch.bfloat16, "k"), _dev_ptr(v, torch.bfloat16, "v"),
-            _dev_ptr(out, torch.bfloat16, "out"), _dev_ptr(lse, torch.float32, "lse"),
-            _dev_ptr(m, torch.int64, "mask_bits"), batches, _dev_ptr(dq, torch.bfloat16, "dq"),
-            _dev_ptr(dk, torch.bfloat16, "dk"), _dev_ptr(dv, torch.bfloat16, "dv"),
-            _dev_ptr(ws, torch.uint8, "workspace"), B, H, N, d, int(blk_q), int(blk_k),
-            float(scale), lay, _stream(stream))
-        _check("sa_bsattn_bwd", st)
-        _used_on(stream, m, dq, dk, dv, ws)
+    dq, dk, dv = q.new_empty(q.shape), q.new_empty(q.shape), q.new_empty(q.shape)
+    ws = _workspace(q, "sa_bsattn_bwd_workspace", B, H, N, d, blk_q, blk_k, batches)
+    _run("sa_bsattn_bwd", dev, stream,
+         (*ptrs, _ptr(m, torch.int64, "mask_bits", dev), batches, dq.data_ptr(), dk.data_ptr(),
+          dv.data_ptr(), ws.data_ptr(), B, H, N, d, blk_q, blk_k, scale, lay), (m, dq, dk, dv, ws))
     return dq, dk, dv
 
 
@@ -770,35 +771,32 @@ def selected_decode(q, k, v, means, lengths, topk, blk, scale=None, stream=None)
     Returns (out bf16 [B, Hq, d], lse float32 [B, Hq], blocks int32 [B, Hkv, topk]).
     """
     torch = _torch()
-    device = _tensors(q=q, k=k, v=v, means=means, lengths=lengths)
+    f32 = torch.float32
+    dev = _device(q, "q")
+    q_ptr = _ptr(q, torch.bfloat16, "q", dev)
     _need(q.dim() == 3 and k.dim() == 4, "q must be [B, Hq, d], k and v [B, Hkv, cap, d]")
+    k_ptr, strides = _rows_ptr(k, "k", dev)
+    v_ptr, v_strides = _rows_ptr(v, "v", dev)
     B, Hq, d = q.shape
-    Hkv, cap = k.shape[1:3]
-    _need(tuple(k.shape) == (B, Hkv, cap, d) and Hkv > 0 and Hq % Hkv == 0,
+    B2, Hkv, cap, d2 = k.shape
+    topk = int(topk)
+    _need(B2 == B and d2 == d and Hkv > 0 and Hq % Hkv == 0,
           "k has shape %s, q %s" % (tuple(k.shape), tuple(q.shape)))
-    _same_shape(k, (v,), ("v",))
+    _need(v.shape == k.shape, "v has shape %s, expected %s" % (tuple(v.shape), tuple(k.shape)))
+    _need(strides[:] == v_strides[:], "k and v must have the same strides")
     _need(blk in (64, 128), "blk must be 64 or 128, got %r" % (blk,))
-    _need(int(topk) >= 1, "topk must be at least 1")
-    _need(tuple(means.shape) == (B, Hkv, -(-cap // blk), d), "means must have shape %s"
+    _need(topk >= 1, "topk must be at least 1")
+    _need(means.shape == (B, Hkv, -(-cap // blk), d), "means must have shape %s"
           % ((B, Hkv, -(-cap // blk), d),))
-    _need(tuple(lengths.shape) == (B,), "lengths must be [B]")
+    _need(lengths.shape == (B,), "lengths must be [B]")
     if scale is None:
         scale = 1.0 / float(d) ** 0.5
-    k_ptr, strides = _rows_ptr(k, "k")
-    v_ptr, v_strides = _rows_ptr(v, "v")
-    _need(list(strides) == list(v_strides), "k and v must have the same strides")
-    lib = load()
-    with _on(device, stream):
-        out = torch.empty((B, Hq, d), dtype=torch.bfloat16, device=device)
-        lse = torch.empty((B, Hq), dtype=torch.float32, device=device)
-        blocks = torch.empty((B, Hkv, int(topk)), dtype=torch.int32, device=device)
-        ws = _workspace(lib, "sa_selected_decode_workspace", device, B, Hq, Hkv, cap, d, blk, topk)
-        st = lib.sa_selected_decode(
-            _dev_ptr(q, torch.bfloat16, "q"), k_ptr, v_ptr, strides,
-            _dev_ptr(means, torch.float32, "means"), _dev_ptr(lengths, torch.int32, "lengths"),
-            _dev_ptr(out, torch.bfloat16, "out"), _dev_ptr(lse, torch.float32, "lse"),
-            _dev_ptr(blocks, torch.int32, "blocks"), _dev_ptr(ws, torch.uint8, "workspace"), B, Hq,
-            Hkv, cap, d, int(blk), int(topk), float(scale), _stream(stream))
-        _check("sa_selected_decode", st)
-        _used_on(stream, out, lse, blocks, ws)
+    out = q.new_empty((B, Hq, d))
+    lse = q.new_empty((B, Hq), dtype=f32)
+    blocks = q.new_empty((B, Hkv, topk), dtype=torch.int32)
+    ws = _workspace(q, "sa_selected_decode_workspace", B, Hq, Hkv, cap, d, blk, topk)
+    _run("sa_selected_decode", dev, stream,
+         (q_ptr, k_ptr, v_ptr, strides, _ptr(means, f32, "means", dev),
+          _ptr(lengths, torch.int32, "lengths", dev), out.data_ptr(), lse.data_ptr(), blocks.data_ptr(),
+          ws.data_ptr(), B, Hq, Hkv, cap, d, blk, topk, scale), (out, lse, blocks, ws))
     return out, lse, blocks

@@ -34,12 +34,14 @@ __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) {
 }
 
 // ---- selection: a workgroup a (sequence, key head) ----
-// Eight lanes take a block's mean, so a wavefront scores eight blocks at a time.
-constexpr int kDecodeSelectThreads = 512;
+// Eight lanes take a block's mean, so a wavefront scores eight blocks at a time, two
+// times over to have enough loads in flight.
+constexpr int kDecodeSelectThreads = 1024;
 
 template <int D>
 __global__ __launch_bounds__(kDecodeSelectThreads) void decode_select_kernel(DecodeArgs a) {
   extern __shared__ uint64_t keys[];  // [n_blk]
+  __shared__ double qparts[kDecodeSelectThreads / D][D];
   __shared__ double qsum[D];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -50,29 +52,43 @@ __global__ __launch_bounds__(kDecodeSelectThreads) void decode_select_kernel(Dec
   const int last = n - 1;
   int32_t* list = a.blocks + (int64_t)bh * a.topk;
   if (last + 1 > a.topk) {  // more blocks than are taken: score and choose
+    constexpr int P = kDecodeSelectThreads / D;  // heads summed side by side
+    const int c = threadIdx.x % D, i0 = threadIdx.x / D;
+    const __bf16* q = (const __bf16*)a.q + ((int64_t)b * a.Hq + (int64_t)h * G) * D + c;
+    double sum = 0.0;
+    for (int i = i0; i < G; i += P) sum += (double)(float)q[(int64_t)i * D];
+    qparts[i0][c] = sum;
+    __syncthreads();
     if (threadIdx.x < D) {
-      const __bf16* q = (const __bf16*)a.q + ((int64_t)b * a.Hq + (int64_t)h * G) * D + threadIdx.x;
-      double t = 0.0;
-      for (int i = 0; i < G; ++i) t += (double)(float)q[(int64_t)i * D];
-      qsum[threadIdx.x] = t;
+      sum = 0.0;
+#pragma unroll
+      for (int i = 0; i < P; ++i) sum += qparts[i][c];
+      qsum[c] = sum;
     }
     __syncthreads();
     const int part = lane & 7;  // columns 4 part + 32 i .. + 3
+    double qs[D / 8];
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) qs[i] = qsum[4 * part + 32 * (i / 4) + i % 4];
     const float* means = a.means + (int64_t)bh * a.n_blk * D + 4 * part;
-    for (int v0 = wave * 8; v0 < last; v0 += kDecodeSelectThreads / 64 * 8) {
-      const int v = v0 + (lane >> 3);
-      const float* m = means + (int64_t)min(v, last - 1) * D;
-      f32x4 x[D / 32];
+    constexpr int U = 2;  // blocks in flight a lane
+    constexpr int kStep = kDecodeSelectThreads / 8;
+    for (int v0 = threadIdx.x >> 3; v0 < last + (int)(threadIdx.x >> 3); v0 += U * kStep) {
+      f32x4 x[U][D / 32];
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) x[i] = *(const f32x4*)(m + 32 * i);
-      double t = 0.0;
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
+        for (int i = 0; i < D / 32; ++i)
+          x[u][i] = *(const f32x4*)(means + (int64_t)min(v0 + u * kStep, last - 1) * D + 32 * i);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) t = fma((double)x[i][e], qsum[4 * part + 32 * i + e], t);
+      for (int u = 0; u < U; ++u) {
+        double t = 0.0;
 #pragma unroll
-      for (int s = 1; s < 8; s *= 2) t += __shfl_xor(t, s, 64);
-      if (part == 0 && v < last) keys[v] = order_key(t);
+        for (int i = 0; i < D / 8; ++i) t = fma((double)x[u][i / 4][i % 4], qs[i], t);
+#pragma unroll
+        for (int s = 1; s < 8; s *= 2) t += __shfl_xor(t, s, 64);
+        if (part == 0 && v0 + u * kStep < last) keys[v0 + u * kStep] = order_key(t);
+      }
     }
     __syncthreads();
   }
@@ -307,29 +323,57 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeAr
   }
 }
 
-// A wavefront a row: its parts' sums, in order.
+// A wavefront a row: its parts' sums, in order.  Lane p holds the weight of part p (64 at a
+// time), which the others read from it.
 template <int D>
 __global__ __launch_bounds__(256) void decode_merge_kernel(DecodeArgs a, int parts) {
+  constexpr int E = D / 64;
   const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= (int64_t)a.B * a.Hq) return;
   const float* ml = a.parts_out + (int64_t)a.B * a.Hq * parts * D + row * parts * 2;
-  const float* po = a.parts_out + row * parts * D;
-  float m = -INFINITY;
-  for (int p = 0; p < parts; ++p) m = fmaxf(m, ml[2 * p]);
-  const float m_exp = fmaxf(m, kLowest);
-  float l = 0.f;
-  float t[D / 64] = {};
-  for (int p = 0; p < parts; ++p) {
-    const float f = fast_exp2(ml[2 * p] - m_exp);
-    l = fmaf(f, ml[2 * p + 1], l);
+  const float* po = a.parts_out + row * parts * D + lane * E;
+  float m = -INFINITY, l = 0.f;
+  float t[E] = {};
+  for (int p0 = 0; p0 < parts; p0 += 64) {
+    const int n = min(64, parts - p0);
+    float mp = -INFINITY, lp = 0.f;
+    if (lane < n) {
+      mp = ml[2 * (p0 + lane)];
+      lp = ml[2 * (p0 + lane) + 1];
+    }
+    float top = mp;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) t[i] = fmaf(f, po[p * D + lane * (D / 64) + i], t[i]);
+    for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s, 64));
+    const float m_new = fmaxf(m, top);
+    const float m_exp = fmaxf(m_new, kLowest);
+    const float keep = fast_exp2(m - m_exp), w = fast_exp2(mp - m_exp);
+    m = m_new;
+    float sum = w * lp;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) sum += __shfl_xor(sum, s, 64);
+    l = fmaf(l, keep, sum);
+#pragma unroll
+    for (int i = 0; i < E; ++i) t[i] *= keep;
+    for (int p = 0; p < n; p += 8) {  // eight parts' sums in flight
+      float x[8][E];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[u][i] = po[(int64_t)(p0 + min(p + u, n - 1)) * D + i];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float f = p + u < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), p + u)) : 0.f;
+        if (p + u < n)
+#pragma unroll
+          for (int i = 0; i < E; ++i) t[i] = fmaf(f, x[u][i], t[i]);
+      }
+    }
   }
   const float inv = l != 0.f ? 1.0f / l : 0.f;
-  __bf16* out = (__bf16*)a.out + row * D + lane * (D / 64);
+  __bf16* out = (__bf16*)a.out + row * D + lane * E;
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) out[i] = (__bf16)(t[i] * inv);
+  for (int i = 0; i < E; ++i) out[i] = (__bf16)(t[i] * inv);
   if (lane == 0) a.lse[row] = l != 0.f ? (m + fast_log2(l)) * kLn2 : -INFINITY;
 }
 

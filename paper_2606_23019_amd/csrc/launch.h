@@ -59,8 +59,17 @@ constexpr int kRopeParts = 1024;
 hipError_t launch_norm_rope(RopeArgs a, hipStream_t stream);
 hipError_t launch_norm_rope_bwd(RopeArgs a, float* dwq, float* dwk, hipStream_t stream);
 
-hipError_t launch_block_means(const void* x, int64_t sb, int64_t sh, int64_t sn, float* means,
-                              int B, int H, int N, int d, int blk, hipStream_t stream);
+// Block means of one tensor, or of two: x (null: none) with element strides of batch, head
+// and token.
+struct MeansArgs {
+  const void* x;
+  int64_t sb, sh, sn;
+  float* means;
+  int blk;
+};
+
+hipError_t launch_block_means(const MeansArgs& q, const MeansArgs& k, int B, int H, int N, int d,
+                              hipStream_t stream);
 
 // Most key blocks of a row that is selected: its keys have to fit in LDS.
 constexpr int kSelectMaxBlocks = 16384;

@@ -225,8 +225,9 @@ SA_API int sa_block_means(const void* x, const int64_t* x_strides, float* means,
   size_t bytes;
   if (!strided(x_strides, {B, H, N}, d, &bytes)) return SA_ERR_INVALID_ARG;
   if (overlap({x, bytes}, {means, (size_t)blocks * d * 4})) return SA_ERR_INVALID_ARG;
-  return status(sa::launch_block_means(x, x_strides[0], x_strides[1], x_strides[2], means, B, H, N, d,
-                                       blk, (hipStream_t)stream));
+  return status(sa::launch_block_means({x, x_strides[0], x_strides[1], x_strides[2], means, blk},
+                                       {nullptr, 0, 0, 0, nullptr, blk}, B, H, N, d,
+                                       (hipStream_t)stream));
 }
 
 SA_API int sa_block_select(const float* q_means, const float* k_means, const uint64_t* candidates,
@@ -292,8 +293,7 @@ SA_API int sa_selected_attn_fwd(const void* q, const void* k, const void* v,
   int32_t* lists = (int32_t*)(ws + w.lists);
   int32_t* order = (int32_t*)(ws + w.order);
   const int64_t sb = (int64_t)H * N * d, sh = (int64_t)N * d;
-  hipError_t e = sa::launch_block_means(q, sb, sh, d, qm, B, H, N, d, blk_q, s);
-  if (e == hipSuccess) e = sa::launch_block_means(k, sb, sh, d, km, B, H, N, d, blk_k, s);
+  hipError_t e = sa::launch_block_means({q, sb, sh, d, qm, blk_q}, {k, sb, sh, d, km, blk_k}, B, H, N, d, s);
   if (e == hipSuccess) {
     sa::SelectArgs a{qm, km, candidates, keep, mask_bits, counts, lists, B, H, n_qb, n_kb, d, topk,
                      candidate_batches > 1, keep_batches > 1};

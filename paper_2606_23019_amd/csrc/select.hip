@@ -22,20 +22,26 @@ typedef double f64x4 __attribute__((ext_vector_type(4)));
 // ---- means ----
 // One block of tokens a workgroup, d / 8 lanes a row, each lane 8 columns in 64 bits.
 // Bound by the HBM bytes of x; a block's 8 to 32 KB are requested in one go.
+struct MeansSide {
+  const void* x;
+  int64_t sb, sh, sn;
+  float* means;
+  int n_blk;
+  int64_t items;
+};
+
 template <int D, int BLK>
-__global__ __launch_bounds__(256) void block_means_kernel(const __bf16* __restrict__ x, int64_t sb,
-                                                          int64_t sh, int64_t sn,
-                                                          float* __restrict__ means, int H, int N,
-                                                          int n_blk) {
+__device__ __forceinline__ void block_mean(const MeansSide& o, int64_t item, int H, int N) {
   constexpr int C = D / 8, R = 256 / C;  // rows a pass
   __shared__ double sums[4][D];
-  const int64_t item = blockIdx.x;
-  const int64_t bh = item / n_blk;
-  const int blk = (int)(item - bh * n_blk);
+  const int64_t bh = item / o.n_blk;
+  const int blk = (int)(item - bh * o.n_blk);
   const int lane = threadIdx.x & 63;
   const int chunk = threadIdx.x % C;
   const int size = min(BLK, N - blk * BLK);
-  const __bf16* from = x + (bh / H) * sb + (bh % H) * sh + (int64_t)blk * BLK * sn + 8 * chunk;
+  const int64_t sn = o.sn;
+  const __bf16* from =
+      (const __bf16*)o.x + (bh / H) * o.sb + (bh % H) * o.sh + (int64_t)blk * BLK * sn + 8 * chunk;
   u32x4 v[BLK / R];
 #pragma unroll
   for (int i = 0; i < BLK / R; ++i) {
@@ -60,8 +66,19 @@ __global__ __launch_bounds__(256) void block_means_kernel(const __bf16* __restri
   __syncthreads();
   if (threadIdx.x < D) {
     const int c = threadIdx.x;
-    means[item * D + c] = (float)((sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c]) / size);
+    o.means[item * D + c] = (float)((sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c]) / size);
   }
+}
+
+// The blocks of one tensor, or of two (queries and keys) one after the other.
+template <int D, int BLK0, int BLK1>
+__global__ __launch_bounds__(256) void block_means_kernel(MeansSide first, MeansSide second, int H,
+                                                          int N) {
+  const int64_t item = blockIdx.x;
+  if (item < first.items)
+    block_mean<D, BLK0>(first, item, H, N);
+  else
+    block_mean<D, BLK1>(second, item - first.items, H, N);
 }
 
 // ---- selection ----
@@ -73,12 +90,12 @@ constexpr int kSelectRows = 16;  // rows of a workgroup: one side of an MFMA til
 // supplies row (or key block) l % 16 and, in step 4 s + e, the column 16 s + 4 (l / 16)
 // + e of both sides, so that its loads are 16 bytes; every key block's sum runs in the
 // same order, so equal blocks score alike.
-template <int D>
-__global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, int rows, int groups) {
+template <int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int rows, int groups) {
   extern __shared__ uint64_t keys_all[];  // [rows][n_pad]
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int waves = blockDim.x / 64;
+  constexpr int waves = THREADS / 64;
   const int n_pad = (a.n_kb + 15) / 16 * 16;
   const int bh = blockIdx.x / groups;
   const int u0 = (blockIdx.x - bh * groups) * rows;
@@ -161,14 +178,24 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, int row
 
 }  // namespace
 
-hipError_t launch_block_means(const void* x, int64_t sb, int64_t sh, int64_t sn, float* means,
-                              int B, int H, int N, int d, int blk, hipStream_t stream) {
-  const int n_blk = (N + blk - 1) / blk;
-  const int64_t grid = (int64_t)B * H * n_blk;
-  auto kernel = d == 128 ? (blk == 128 ? block_means_kernel<128, 128> : block_means_kernel<128, 64>)
-                         : (blk == 128 ? block_means_kernel<64, 128> : block_means_kernel<64, 64>);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, stream, (const __bf16*)x, sb, sh,
-                     sn, means, H, N, n_blk);
+hipError_t launch_block_means(const MeansArgs& q, const MeansArgs& k, int B, int H, int N, int d,
+                              hipStream_t stream) {
+  auto side = [&](const MeansArgs& a) {
+    const int n_blk = (N + a.blk - 1) / a.blk;
+    return MeansSide{a.x, a.sb, a.sh, a.sn, a.means, n_blk, a.x ? (int64_t)B * H * n_blk : 0};
+  };
+  const MeansSide first = side(q), second = side(k);
+  const dim3 grid((unsigned)(first.items + second.items));
+  auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, first, second, H, N);
+  };
+  const bool q128 = q.blk == 128, k128 = k.blk == 128;
+  if (d == 128)
+    q128 ? (k128 ? run(block_means_kernel<128, 128, 128>) : run(block_means_kernel<128, 128, 64>))
+         : (k128 ? run(block_means_kernel<128, 64, 128>) : run(block_means_kernel<128, 64, 64>));
+  else
+    q128 ? (k128 ? run(block_means_kernel<64, 128, 128>) : run(block_means_kernel<64, 128, 64>))
+         : (k128 ? run(block_means_kernel<64, 64, 128>) : run(block_means_kernel<64, 64, 64>));
   return hipGetLastError();
 }
 
@@ -180,13 +207,16 @@ hipError_t launch_block_select(const SelectArgs& a, hipStream_t stream) {
   const int groups = (a.n_qb + rows - 1) / rows;
   const int64_t grid = (int64_t)a.B * a.H * groups;
   const int lds = rows * n_pad * 8;
-  auto kernel = a.d == 128 ? block_select_kernel<128> : block_select_kernel<64>;
+  // up to a workgroup a compute unit, 16 wavefronts: a row each; more share the units
+  const bool few = grid <= 256;
+  auto kernel = a.d == 128 ? (few ? block_select_kernel<128, 1024> : block_select_kernel<128, 512>)
+                           : (few ? block_select_kernel<64, 1024> : block_select_kernel<64, 512>);
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute((const void*)kernel,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), lds, stream, a, rows, groups);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(few ? 1024 : 512), lds, stream, a, rows, groups);
   return hipGetLastError();
 }
 

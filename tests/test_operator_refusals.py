@@ -148,6 +148,19 @@ def test_workspaces_of_refused_sizes_are_zero(lib):
     assert lib.sa_bsattn_bwd_workspace(1, 1, 64, 64, 64, 64, 1) % 256 == 0
 
 
+def FakeGpu(t, index=0):
+    """A tensor that says it is on a GPU."""
+    import torch
+
+    class OnGpu(torch.Tensor):
+        is_cuda = True
+        device = torch.device("cuda", index)
+
+        def get_device(self):
+            return index
+    return t.as_subclass(OnGpu)
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     import torch
     x = torch.zeros((1, 4, 2, 64), dtype=torch.bfloat16)
@@ -157,6 +170,17 @@ def test_binding_refuses_what_the_library_cannot_see():
         binding.block_means([1.0], 64)
     with pytest.raises(ValueError, match="on the GPU"):
         binding.bsattn_bwd(x, x, x, x, x, x, torch.zeros((2, 1, 1), dtype=torch.int64), 64, 64)
+    with pytest.raises(ValueError, match="on the GPU"):
+        binding._ptr(x, torch.bfloat16, "x", 0)
+    with pytest.raises(TypeError, match="must be torch.float32"):
+        binding._ptr(FakeGpu(x), torch.float32, "x", 0)
+    with pytest.raises(ValueError, match="contiguous"):
+        binding._ptr(FakeGpu(x.transpose(1, 2)), torch.bfloat16, "x", 0)
+    with pytest.raises(ValueError, match="is on GPU 1"):
+        binding._ptr(FakeGpu(x, 1), torch.bfloat16, "x", 0)
+    with pytest.raises(ValueError, match="is on GPU 1"):
+        binding._rows_ptr(FakeGpu(x, 1), "x", 0)
+    assert binding._ptr(FakeGpu(x), torch.bfloat16, "x", 0) == x.data_ptr()
     with pytest.raises(ValueError, match="pairs must be"):
         binding._named(binding._PAIRS, "both", "pairs")
     for shape in ((1, 1, 1), (2, 2, 1), (2, 3, 1, 1), (2, 1, 1, 1, 1)):
@@ -165,7 +189,8 @@ def test_binding_refuses_what_the_library_cannot_see():
     for ok, n in (((2, 1, 1), 1), ((1, 2, 1, 1), 1), ((3, 2, 1, 1), 3)):
         assert binding._mask_arg(torch.zeros(ok, dtype=torch.int64), 3, 2, 1, 1, "mask_bits")[1] == n
     with pytest.raises(ValueError, match="16-byte"):
-        binding._rows_ptr(torch.zeros((1, 4, 2, 65), dtype=torch.bfloat16)[..., :64], "x")
+        binding._rows_ptr(FakeGpu(torch.zeros((1, 4, 2, 65), dtype=torch.bfloat16)[..., :64]), "x", 0)
     with pytest.raises(ValueError, match="last dimension"):
-        binding._rows_ptr(x.transpose(2, 3), "x")
-    assert list(binding._rows_ptr(x.expand(1, 4, 2, 64).transpose(1, 2), "x")[1]) == [0, 64, 128]
+        binding._rows_ptr(FakeGpu(x.transpose(2, 3)), "x", 0)
+    assert list(binding._rows_ptr(FakeGpu(x.transpose(1, 2)), "x", 0)[1]) == [0, 64, 128]
+    assert list(binding._rows_ptr(FakeGpu(x[:, :1].expand(3, 4, 2, 64)), "x", 0)[1]) == [0, 0, 64]
