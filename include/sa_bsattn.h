@@ -325,7 +325,7 @@ SA_API int sa_bsattn_plan_destroy(sa_plan_t plan);
  * its blocks, its gradients, and its form for single tokens.  None allocates,
  * synchronises or keeps anything: workspaces are the caller's, 256-byte aligned,
  * of the size that the _workspace function gives (0 for sizes that the call
- * refuses), need no initial values, and are free again when the call's work on
+ * refuses and where it needs none: NULL will do), need no initial values, and are free again when the call's work on
  * its stream is done.  Calls that overlap in time need workspaces of their own;
  * every call may be captured into a graph, whose replays need theirs.  The same
  * call gives the same bits: no sum goes by the order of arrival.

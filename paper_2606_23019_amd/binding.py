@@ -176,7 +176,8 @@ def _used_on(stream, *tensors):
     if stream == torch.cuda.current_stream():
         return
     for t in tensors:
-        t.record_stream(stream)
+        if t is not None:
+            t.record_stream(stream)
 
 
 def mask_to_device(mask_bits, device="cuda"):
@@ -512,6 +513,21 @@ def _ptr(t, dtype, name, dev):
     return t.data_ptr()
 
 
+def _ptrs(dev, dtype, **named):
+    """Addresses of contiguous tensors of one type on GPU ``dev``; None stays None."""
+    out = []
+    for name, t in named.items():
+        if t is None:
+            out.append(None)
+            continue
+        try:
+            good = t.dtype is dtype and t.is_contiguous() and t.get_device() == dev
+        except AttributeError:
+            good = False
+        out.append(t.data_ptr() if good else _ptr(t, dtype, name, dev))
+    return out
+
+
 @functools.lru_cache(maxsize=256)
 def _strides(*s):
     return (ctypes.c_int64 * 3)(*s)
@@ -540,7 +556,7 @@ def _run(fn, dev, stream, args, made):
     tensors allocated for the call."""
     torch = _torch()
     if stream is None and torch.cuda.current_device() == dev:
-        st = getattr(load(), fn)(*args, torch.cuda.current_stream().cuda_stream)
+        st = getattr(_LIB or load(), fn)(*args, _current_stream(dev))
     else:
         _need(stream is None or stream.device_index == dev, "stream is not of GPU %d" % dev)
         with torch.cuda.device(dev):
@@ -550,9 +566,22 @@ def _run(fn, dev, stream, args, made):
         raise SAError(fn, st)
 
 
-def _workspace(like, fn, *sizes):
+def _current_stream(dev):
+    """Handle of the current stream of GPU ``dev``; torch's own launchers ask for it this way, a
+    Stream object takes 2.6 us to make."""
     torch = _torch()
-    return like.new_empty(max(1, getattr(load(), fn)(*sizes)), dtype=torch.uint8)
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(dev) if get else torch.cuda.current_stream(dev).cuda_stream
+
+
+def _workspace(like, fn, *sizes):
+    """A workspace for the call, None where it needs none (or refuses the sizes)."""
+    n = getattr(_LIB or load(), fn)(*sizes)
+    return like.new_empty(n, dtype=_torch().uint8) if n else None
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
 
 
 def _mask_arg(m, B, H, n_qb, n_kb, name):
@@ -602,19 +631,17 @@ def qk_norm_rope(q, k, wq, wk, cos, sin, positions=None, eps=1e-6, pairs="interl
     (``layout`` "bhnd", as the attention reads them) or [B, N, H, d] ("bnhd").
     """
     torch = _torch()
-    f32 = torch.float32
     dev = _device(q, "q")
     q_ptr, q_str = _rows_ptr(q, "q", dev)
     k_ptr, k_str = _rows_ptr(k, "k", dev)
-    ptrs = (_ptr(wq, f32, "wq", dev), _ptr(wk, f32, "wk", dev), _ptr(cos, f32, "cos", dev),
-            _ptr(sin, f32, "sin", dev),
-            None if positions is None else _ptr(positions, torch.int32, "positions", dev))
+    ptrs = _ptrs(dev, torch.float32, wq=wq, wk=wk, cos=cos, sin=sin)
+    pos = None if positions is None else _ptr(positions, torch.int32, "positions", dev)
     B, N, Hq, Hk, d, rot, n_pos, pr, lay = _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs,
                                                         layout)
     q_out = q.new_empty(_heads_shape(lay, B, N, Hq, d))
     k_out = q.new_empty(_heads_shape(lay, B, N, Hk, d))
     _run("sa_qk_norm_rope", dev, stream,
-         (q_ptr, q_str, k_ptr, k_str, *ptrs, q_out.data_ptr(), k_out.data_ptr(), B, N, Hq, Hk, d, rot,
+         (q_ptr, q_str, k_ptr, k_str, *ptrs, pos, q_out.data_ptr(), k_out.data_ptr(), B, N, Hq, Hk, d, rot,
           n_pos, eps, pr, lay), (q_out, k_out))
     return q_out, k_out
 
@@ -627,14 +654,12 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, wq, wk, cos, sin, positions=None, eps
     (dq bf16 [B, N, Hq, d], dk bf16 [B, N, Hk, d], dwq float32 [d], dwk float32 [d]).
     """
     torch = _torch()
-    f32, b16 = torch.float32, torch.bfloat16
     dev = _device(q, "q")
     q_ptr, q_str = _rows_ptr(q, "q", dev)
     k_ptr, k_str = _rows_ptr(k, "k", dev)
-    grads = _ptr(dq_out, b16, "dq_out", dev), _ptr(dk_out, b16, "dk_out", dev)
-    ptrs = (_ptr(wq, f32, "wq", dev), _ptr(wk, f32, "wk", dev), _ptr(cos, f32, "cos", dev),
-            _ptr(sin, f32, "sin", dev),
-            None if positions is None else _ptr(positions, torch.int32, "positions", dev))
+    grads = _ptrs(dev, torch.bfloat16, dq_out=dq_out, dk_out=dk_out)
+    ptrs = _ptrs(dev, torch.float32, wq=wq, wk=wk, cos=cos, sin=sin)
+    pos = None if positions is None else _ptr(positions, torch.int32, "positions", dev)
     B, N, Hq, Hk, d, rot, n_pos, pr, lay = _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs,
                                                         layout)
     for t, H, name in ((dq_out, Hq, "dq_out"), (dk_out, Hk, "dk_out")):
@@ -644,8 +669,8 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, wq, wk, cos, sin, positions=None, eps
     dwq, dwk = wq.new_empty(d), wq.new_empty(d)
     ws = _workspace(q, "sa_qk_norm_rope_bwd_workspace", d)
     _run("sa_qk_norm_rope_bwd", dev, stream,
-         (*grads, q_ptr, q_str, k_ptr, k_str, *ptrs, dq.data_ptr(), dk.data_ptr(), dwq.data_ptr(),
-          dwk.data_ptr(), ws.data_ptr(), B, N, Hq, Hk, d, rot, n_pos, eps, pr, lay),
+         (*grads, q_ptr, q_str, k_ptr, k_str, *ptrs, pos, dq.data_ptr(), dk.data_ptr(), dwq.data_ptr(),
+          dwk.data_ptr(), _address(ws), B, N, Hq, Hk, d, rot, n_pos, eps, pr, lay),
          (dq, dk, dwq, dwk, ws))
     return dq, dk, dwq, dwk
 
@@ -675,8 +700,7 @@ def block_select(q_means, k_means, topk, candidates=None, keep=None, stream=None
     """
     torch = _torch()
     dev = _device(q_means, "q_means")
-    q_ptr = _ptr(q_means, torch.float32, "q_means", dev)
-    k_ptr = _ptr(k_means, torch.float32, "k_means", dev)
+    ptrs = _ptrs(dev, torch.float32, q_means=q_means, k_means=k_means)
     _need(q_means.dim() == 4 and k_means.dim() == 4, "q_means and k_means must be [B, H, blocks, d]")
     B, H, n_qb, d = q_means.shape
     B2, H2, n_kb, d2 = k_means.shape
@@ -684,11 +708,10 @@ def block_select(q_means, k_means, topk, candidates=None, keep=None, stream=None
           % (tuple(k_means.shape), B, H, d))
     candidates, cb = _mask_arg(candidates, B, H, n_qb, n_kb, "candidates")
     keep, kb = _mask_arg(keep, B, H, n_qb, n_kb, "keep")
+    c_ptr, k_ptr = _ptrs(dev, torch.int64, candidates=candidates, keep=keep)
     mask = q_means.new_empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64)
     _run("sa_block_select", dev, stream,
-         (q_ptr, k_ptr, None if candidates is None else _ptr(candidates, torch.int64, "candidates", dev),
-          cb, None if keep is None else _ptr(keep, torch.int64, "keep", dev), kb, mask.data_ptr(), None,
-          None, B, H, n_qb, n_kb, d, int(topk)), (mask,))
+         (*ptrs, c_ptr, cb, k_ptr, kb, mask.data_ptr(), None, None, B, H, n_qb, n_kb, d, int(topk)), (mask,))
     return mask
 
 
@@ -701,9 +724,8 @@ def selected_attn_fwd(q, k, v, blk_q, blk_k, topk, candidates=None, keep=None, s
     the mask is what ``bsattn_bwd`` takes.
     """
     torch = _torch()
-    b16 = torch.bfloat16
     dev = _device(q, "q")
-    ptrs = _ptr(q, b16, "q", dev), _ptr(k, b16, "k", dev), _ptr(v, b16, "v", dev)
+    ptrs = _ptrs(dev, torch.bfloat16, q=q, k=k, v=v)
     _need(q.dim() == 4, "q must be [B, H, N, d]")
     B, H, N, d = q.shape
     _same_shape(q, (k, v), ("k", "v"))
@@ -711,6 +733,7 @@ def selected_attn_fwd(q, k, v, blk_q, blk_k, topk, candidates=None, keep=None, s
     n_qb, n_kb = -(-N // blk_q), -(-N // blk_k)
     candidates, cb = _mask_arg(candidates, B, H, n_qb, n_kb, "candidates")
     keep, kb = _mask_arg(keep, B, H, n_qb, n_kb, "keep")
+    c_ptr, k_ptr = _ptrs(dev, torch.int64, candidates=candidates, keep=keep)
     if scale is None:
         scale = 1.0 / float(d) ** 0.5
     out = q.new_empty((B, H, N, d))
@@ -718,9 +741,7 @@ def selected_attn_fwd(q, k, v, blk_q, blk_k, topk, candidates=None, keep=None, s
     mask = q.new_empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64)
     ws = _workspace(q, "sa_selected_attn_workspace", B, H, N, d, blk_q, blk_k)
     _run("sa_selected_attn_fwd", dev, stream,
-         (*ptrs, None if candidates is None else _ptr(candidates, torch.int64, "candidates", dev), cb,
-          None if keep is None else _ptr(keep, torch.int64, "keep", dev), kb, out.data_ptr(),
-          lse.data_ptr(), mask.data_ptr(), ws.data_ptr(), B, H, N, d, blk_q, blk_k, int(topk), scale),
+         (*ptrs, c_ptr, cb, k_ptr, kb, out.data_ptr(), lse.data_ptr(), mask.data_ptr(), _address(ws), B, H, N, d, blk_q, blk_k, int(topk), scale),
          (out, lse, mask, ws))
     return out, lse, mask
 
@@ -735,10 +756,9 @@ def bsattn_bwd(dout, q, k, v, out, lse, mask_bits, blk_q, blk_k, scale=None, lay
     ``selected_attn_fwd`` returns them.
     """
     torch = _torch()
-    b16 = torch.bfloat16
     dev = _device(q, "q")
-    ptrs = (_ptr(dout, b16, "dout", dev), _ptr(q, b16, "q", dev), _ptr(k, b16, "k", dev),
-            _ptr(v, b16, "v", dev), _ptr(out, b16, "out", dev), _ptr(lse, torch.float32, "lse", dev))
+    ptrs = _ptrs(dev, torch.bfloat16, dout=dout, q=q, k=k, v=v, out=out)
+    ptrs += _ptrs(dev, torch.float32, lse=lse)
     lay = _named(_LAYOUTS, layout, "layout")
     _need(q.dim() == 4, "q must have four dimensions")
     if lay == SA_LAYOUT_BHND:
@@ -757,7 +777,7 @@ def bsattn_bwd(dout, q, k, v, out, lse, mask_bits, blk_q, blk_k, scale=None, lay
     ws = _workspace(q, "sa_bsattn_bwd_workspace", B, H, N, d, blk_q, blk_k, batches)
     _run("sa_bsattn_bwd", dev, stream,
          (*ptrs, _ptr(m, torch.int64, "mask_bits", dev), batches, dq.data_ptr(), dk.data_ptr(),
-          dv.data_ptr(), ws.data_ptr(), B, H, N, d, blk_q, blk_k, scale, lay), (m, dq, dk, dv, ws))
+          dv.data_ptr(), _address(ws), B, H, N, d, blk_q, blk_k, scale, lay), (m, dq, dk, dv, ws))
     return dq, dk, dv
 
 
@@ -771,7 +791,6 @@ def selected_decode(q, k, v, means, lengths, topk, blk, scale=None, stream=None)
     Returns (out bf16 [B, Hq, d], lse float32 [B, Hq], blocks int32 [B, Hkv, topk]).
     """
     torch = _torch()
-    f32 = torch.float32
     dev = _device(q, "q")
     q_ptr = _ptr(q, torch.bfloat16, "q", dev)
     _need(q.dim() == 3 and k.dim() == 4, "q must be [B, Hq, d], k and v [B, Hkv, cap, d]")
@@ -792,11 +811,11 @@ def selected_decode(q, k, v, means, lengths, topk, blk, scale=None, stream=None)
     if scale is None:
         scale = 1.0 / float(d) ** 0.5
     out = q.new_empty((B, Hq, d))
-    lse = q.new_empty((B, Hq), dtype=f32)
+    lse = q.new_empty((B, Hq), dtype=torch.float32)
     blocks = q.new_empty((B, Hkv, topk), dtype=torch.int32)
     ws = _workspace(q, "sa_selected_decode_workspace", B, Hq, Hkv, cap, d, blk, topk)
     _run("sa_selected_decode", dev, stream,
-         (q_ptr, k_ptr, v_ptr, strides, _ptr(means, f32, "means", dev),
+         (q_ptr, k_ptr, v_ptr, strides, _ptr(means, torch.float32, "means", dev),
           _ptr(lengths, torch.int32, "lengths", dev), out.data_ptr(), lse.data_ptr(), blocks.data_ptr(),
-          ws.data_ptr(), B, Hq, Hkv, cap, d, blk, topk, scale), (out, lse, blocks, ws))
+          _address(ws), B, Hq, Hkv, cap, d, blk, topk, scale), (out, lse, blocks, ws))
     return out, lse, blocks

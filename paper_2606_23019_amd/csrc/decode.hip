@@ -8,7 +8,8 @@
 //   out, lse = softmax attention of the group's G queries over the tokens < L of the
 //              chosen blocks.
 //
-// Two or three launches: decode_select_kernel writes the chosen blocks in ascending
+// One launch where few blocks are taken (decode_fused_kernel), else two or three:
+// decode_select_kernel writes the chosen blocks in ascending
 // order, decode_attn_kernel walks them in `parts` runs, decode_merge_kernel puts the
 // runs together where there is more than one.
 //
@@ -36,93 +37,104 @@ __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) {
 // ---- selection: a workgroup a (sequence, key head) ----
 // Eight lanes take a block's mean, so a wavefront scores eight blocks at a time, two
 // times over to have enough loads in flight.
+template <int D, int THREADS>
+struct ChooseLds {
+  double qparts[THREADS / D][D];
+  double qsum[D];
+};
+
+// The chosen blocks of (b, h), in ascending order, to each of `put`'s calls (place, block):
+// places below the returned number.  Every thread of the workgroup calls this; wavefront 0
+// does the choosing, so what it puts into LDS needs a barrier.
+template <int D, int THREADS, typename Put>
+__device__ __forceinline__ int choose(const DecodeArgs& a, int b, int h, uint64_t* keys,
+                                      ChooseLds<D, THREADS>& lds, Put put) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.Hq / a.Hkv;
+  const int n = (length_of(a, b) + a.blk - 1) / a.blk;  // blocks with a token
+  const int last = n - 1;
+  if (n <= a.topk) {  // all of them
+    for (int v = threadIdx.x; v < n; v += THREADS) put(v, v);
+    return n;
+  }
+  constexpr int P = THREADS / D;  // heads summed side by side
+  const int c = threadIdx.x % D, i0 = threadIdx.x / D;
+  const __bf16* q = (const __bf16*)a.q + ((int64_t)b * a.Hq + (int64_t)h * G) * D + c;
+  double sum = 0.0;
+  for (int i = i0; i < G; i += P) sum += (double)(float)q[(int64_t)i * D];
+  lds.qparts[i0][c] = sum;
+  __syncthreads();
+  if (threadIdx.x < D) {
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) sum += lds.qparts[i][c];
+    lds.qsum[c] = sum;
+  }
+  __syncthreads();
+  const int part = lane & 7;  // columns 4 part + 32 i .. + 3
+  double qs[D / 8];
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) qs[i] = lds.qsum[4 * part + 32 * (i / 4) + i % 4];
+  const float* means = a.means + ((int64_t)b * a.Hkv + h) * a.n_blk * D + 4 * part;
+  constexpr int U = 2;  // blocks in flight a lane
+  constexpr int kStep = THREADS / 8;
+  for (int v0 = threadIdx.x >> 3; v0 < last + (int)(threadIdx.x >> 3); v0 += U * kStep) {
+    f32x4 x[U][D / 32];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+        x[u][i] = *(const f32x4*)(means + (int64_t)min(v0 + u * kStep, last - 1) * D + 32 * i);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      double t = 0.0;
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) t = fma((double)x[u][i / 4][i % 4], qs[i], t);
+#pragma unroll
+      for (int s = 1; s < 8; s *= 2) t += __shfl_xor(t, s, 64);
+      if (part == 0 && v0 + u * kStep < last) keys[v0 + u * kStep] = order_key(t);
+    }
+  }
+  __syncthreads();
+  if (wave != 0) return a.topk;
+  const int words = (last + 63) / 64;
+  Border edge;
+  if (words <= 4)
+    edge = border_of<4>(keys, last, a.topk - 1, lane);
+  else if (words <= 20)
+    edge = border_of<20>(keys, last, a.topk - 1, lane);
+  else
+    edge = border_of_long(keys, last, a.topk - 1, lane);
+  const uint64_t below = (1ull << lane) - 1ull;
+  int done = 0;
+  for (int w = 0; w < words; ++w) {
+    const uint64_t key = 64 * w + lane < last ? keys[64 * w + lane] : 0;
+    uint64_t word = __ballot(key >= edge.lo);
+    if (edge.ties >= 0) {
+      const uint64_t same = __ballot(key == edge.lo);
+      const bool first = key == edge.lo && (int)__popcll(same & below) < edge.ties;
+      word = __ballot(key > edge.lo || first);
+      edge.ties = max(0, edge.ties - (int)__popcll(same));
+    }
+    if ((word >> lane) & 1ull) put(done + (int)__popcll(word & below), 64 * w + lane);
+    done += __popcll(word);
+  }
+  if (lane == 0) put(done, last);
+  return a.topk;
+}
+
 constexpr int kDecodeSelectThreads = 1024;
 
 template <int D>
 __global__ __launch_bounds__(kDecodeSelectThreads) void decode_select_kernel(DecodeArgs a) {
   extern __shared__ uint64_t keys[];  // [n_blk]
-  __shared__ double qparts[kDecodeSelectThreads / D][D];
-  __shared__ double qsum[D];
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ ChooseLds<D, kDecodeSelectThreads> lds;
   const int bh = blockIdx.x;
-  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
-  const int G = a.Hq / a.Hkv;
-  const int n = (length_of(a, b) + a.blk - 1) / a.blk;  // blocks with a token
-  const int last = n - 1;
   int32_t* list = a.blocks + (int64_t)bh * a.topk;
-  if (last + 1 > a.topk) {  // more blocks than are taken: score and choose
-    constexpr int P = kDecodeSelectThreads / D;  // heads summed side by side
-    const int c = threadIdx.x % D, i0 = threadIdx.x / D;
-    const __bf16* q = (const __bf16*)a.q + ((int64_t)b * a.Hq + (int64_t)h * G) * D + c;
-    double sum = 0.0;
-    for (int i = i0; i < G; i += P) sum += (double)(float)q[(int64_t)i * D];
-    qparts[i0][c] = sum;
-    __syncthreads();
-    if (threadIdx.x < D) {
-      sum = 0.0;
-#pragma unroll
-      for (int i = 0; i < P; ++i) sum += qparts[i][c];
-      qsum[c] = sum;
-    }
-    __syncthreads();
-    const int part = lane & 7;  // columns 4 part + 32 i .. + 3
-    double qs[D / 8];
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) qs[i] = qsum[4 * part + 32 * (i / 4) + i % 4];
-    const float* means = a.means + (int64_t)bh * a.n_blk * D + 4 * part;
-    constexpr int U = 2;  // blocks in flight a lane
-    constexpr int kStep = kDecodeSelectThreads / 8;
-    for (int v0 = threadIdx.x >> 3; v0 < last + (int)(threadIdx.x >> 3); v0 += U * kStep) {
-      f32x4 x[U][D / 32];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-          x[u][i] = *(const f32x4*)(means + (int64_t)min(v0 + u * kStep, last - 1) * D + 32 * i);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        double t = 0.0;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) t = fma((double)x[u][i / 4][i % 4], qs[i], t);
-#pragma unroll
-        for (int s = 1; s < 8; s *= 2) t += __shfl_xor(t, s, 64);
-        if (part == 0 && v0 + u * kStep < last) keys[v0 + u * kStep] = order_key(t);
-      }
-    }
-    __syncthreads();
-  }
-  if (wave != 0) return;
-  int done = 0;
-  if (last + 1 > a.topk) {
-    const int words = (last + 63) / 64;
-    Border edge;
-    if (words <= 4)
-      edge = border_of<4>(keys, last, a.topk - 1, lane);
-    else if (words <= 20)
-      edge = border_of<20>(keys, last, a.topk - 1, lane);
-    else
-      edge = border_of_long(keys, last, a.topk - 1, lane);
-    const uint64_t below = (1ull << lane) - 1ull;
-    for (int w = 0; w < words; ++w) {
-      const uint64_t key = 64 * w + lane < last ? keys[64 * w + lane] : 0;
-      uint64_t word = __ballot(key >= edge.lo);
-      if (edge.ties >= 0) {
-        const uint64_t same = __ballot(key == edge.lo);
-        const bool first = key == edge.lo && (int)__popcll(same & below) < edge.ties;
-        word = __ballot(key > edge.lo || first);
-        edge.ties = max(0, edge.ties - (int)__popcll(same));
-      }
-      if ((word >> lane) & 1ull) list[done + __popcll(word & below)] = 64 * w + lane;
-      done += __popcll(word);
-    }
-    if (lane == 0) list[done] = last;
-    ++done;
-  } else {
-    for (int v = lane; v <= last; v += 64) list[v] = v;
-    done = last + 1;
-  }
-  for (int i = done + lane; i < a.topk; i += 64) list[i] = -1;
+  const int n = choose<D, kDecodeSelectThreads>(a, bh / a.Hkv, bh % a.Hkv, keys, lds,
+                                                [&](int at, int v) { list[at] = v; });
+  for (int i = n + threadIdx.x; i < a.topk; i += kDecodeSelectThreads) list[i] = -1;
 }
 
 // ---- attention ----
@@ -131,6 +143,17 @@ __global__ __launch_bounds__(kDecodeSelectThreads) void decode_select_kernel(Dec
 // C[4 (l / 16) + i][l % 16].
 __device__ __forceinline__ f32x4 mfma16x16x32(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Max and sum over lanes l, l ^ 16, l ^ 32 and l ^ 48, by row exchanges in the vector ALU
+// (see pair_max).
+__device__ __forceinline__ float quad_max(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
 // XOR of the 16-byte chunk index of a value tile's row: rows read together by a
@@ -143,7 +166,6 @@ __device__ __forceinline__ int vswz(int r) {
     return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
 
-constexpr int kDecodeWaves = 4;
 constexpr int kDecodeGroup = 16;  // query heads of a workgroup: one side of an MFMA tile
 
 // A wavefront takes units of 32 keys: S^T = K Q^T with keys straight from memory
@@ -151,33 +173,30 @@ constexpr int kDecodeGroup = 16;  // query heads of a workgroup: one side of an 
 // product's operand), O^T += V^T P^T with the values through LDS and the transposing
 // read.  Keys of the next unit are requested when S is done, its values when this
 // unit's are in LDS.  Each wavefront has its own maximum and sums; they meet in LDS.
-template <int D>
-__global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeArgs a, int parts,
-                                                                        int groups) {
+template <int D, int WAVES>
+struct AttendLds {
+  __attribute__((aligned(1024))) __bf16 Vs[WAVES][32 * D];
+  float stats[WAVES][2][16];
+};
+
+// Entries i0 .. i1 - 1 of the list of chosen blocks, block_at(i) for entry i - i0, by the
+// workgroup's WAVES wavefronts; part `part` of `parts`.
+template <int D, int WAVES, typename BlockAt>
+__device__ __forceinline__ void attend(const DecodeArgs& a, int b, int h, int hg, int part, int parts,
+                                       int i0, int i1, BlockAt block_at, AttendLds<D, WAVES>& lds) {
   constexpr int C = D / 8;        // 16-byte chunks of a row
   constexpr int R = 64 / C;       // rows of a load
   constexpr int kVLoads = 32 / R;
-  __shared__ __attribute__((aligned(1024))) __bf16 Vs[kDecodeWaves][32 * D];
-  __shared__ float stats[kDecodeWaves][2][16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int part = blockIdx.x % parts;
-  const int rest = blockIdx.x / parts;
-  const int hg = rest % groups;
-  const int bh = rest / groups;
-  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
   const int G = a.Hq / a.Hkv;
   const int g0 = hg * kDecodeGroup;
   const int heads = min(kDecodeGroup, G - g0);
   const int len = length_of(a, b);
   const int n = (len + a.blk - 1) / a.blk;
-  const int cnt = min(a.topk, n);
-  const int per = (cnt + parts - 1) / parts;
-  const int i0 = min(part * per, cnt), i1 = min(i0 + per, cnt);
   const int shift = a.blk == 128 ? 2 : 1;  // units of a block: 4 or 2
   const int units = (i1 - i0) << shift;
-  const const_ints list = constant(a.blocks) + (int64_t)bh * a.topk + i0;
 
   bf16x8 qf[D / 32];
 #pragma unroll
@@ -192,7 +211,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeAr
   const float c_log2 = a.scale * kLog2e;
 
   auto key0_of = [&](int u) {  // first token of unit u; blocks are below n
-    const int blk = min(max(list[u >> shift], 0), n - 1);
+    const int blk = min(max(block_at(u >> shift), 0), n - 1);
     return blk * a.blk + ((u & ((1 << shift) - 1)) << 5);
   };
   bf16x8 kf[2][D / 32];
@@ -216,7 +235,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeAr
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) o[i] = f32x4{};
   float m_run = -INFINITY, l_run = 0.f;
-  __bf16* vs = Vs[wave];
+  __bf16* vs = lds.Vs[wave];
   int u = wave;
   int key0 = 0;
   if (u < units) {
@@ -224,14 +243,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeAr
     load_k(key0);
     load_v(key0);
   }
-  for (; u < units; u += kDecodeWaves) {
+  for (; u < units; u += WAVES) {
     f32x4 s2[2] = {};
 #pragma unroll
     for (int s = 0; s < D / 32; ++s)
 #pragma unroll
       for (int t = 0; t < 2; ++t) s2[t] = mfma16x16x32(kf[t][s], qf[s], s2[t]);
-    const bool more = u + kDecodeWaves < units;
-    const int key1 = more ? key0_of(u + kDecodeWaves) : key0;
+    const bool more = u + WAVES < units;
+    const int key1 = more ? key0_of(u + WAVES) : key0;
     if (more) load_k(key1);
     float x[8];  // key key0 + 8 g + e, query l16
     float mx = -INFINITY;
@@ -240,8 +259,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeAr
       x[e] = key0 + 8 * g + e < len ? s2[e >> 2][e & 3] : -INFINITY;
       mx = fmaxf(mx, x[e]);
     }
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c_log2;
+    mx = quad_max(mx) * c_log2;
     const float m_new = fmaxf(m_run, mx);
     // a maximum of -inf (nothing seen yet, or logits of -inf only) weighs nothing
     const float m_exp = fmaxf(m_new, kLowest);
@@ -275,16 +293,15 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeAr
     }
     key0 = key1;
   }
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
+  l_run = quad_sum(l_run);
 
   // Put the wavefronts together: out = sum_w exp2(m_w - m) O_w over the same sum of l_w.
-  float* os = (float*)Vs[0];  // [wave][query][D / 4 chunks, XOR of the query] of 4 floats
-  static_assert(sizeof(Vs) >= sizeof(float) * kDecodeWaves * 16 * D, "the value tiles hold the sums");
+  float* os = (float*)lds.Vs[0];  // [wave][query][D / 4 chunks, XOR of the query] of 4 floats
+  static_assert(sizeof(lds.Vs) >= sizeof(float) * WAVES * 16 * D, "the value tiles hold the sums");
   __syncthreads();
   if (g == 0) {
-    stats[wave][0][l16] = m_run;
-    stats[wave][1][l16] = l_run;
+    lds.stats[wave][0][l16] = m_run;
+    lds.stats[wave][1][l16] = l_run;
   }
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {  // o[i][e] is column 16 i + 4 g + e of query l16
@@ -292,18 +309,18 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeAr
     *(SA_LDS f32x4*)(os + (wave * 16 + l16) * D + 4 * ch) = o[i];
   }
   __syncthreads();
-  for (int c = threadIdx.x; c < heads * (D / 4); c += 64 * kDecodeWaves) {
+  for (int c = threadIdx.x; c < heads * (D / 4); c += 64 * WAVES) {
     const int qi = c / (D / 4), ch = c % (D / 4);
     float m = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kDecodeWaves; ++w) m = fmaxf(m, stats[w][0][qi]);
+    for (int w = 0; w < WAVES; ++w) m = fmaxf(m, lds.stats[w][0][qi]);
     const float m_exp = fmaxf(m, kLowest);
     float l = 0.f;
     f32x4 t = {};
 #pragma unroll
-    for (int w = 0; w < kDecodeWaves; ++w) {
-      const float f = fast_exp2(stats[w][0][qi] - m_exp);
-      l = fmaf(f, stats[w][1][qi], l);
+    for (int w = 0; w < WAVES; ++w) {
+      const float f = fast_exp2(lds.stats[w][0][qi] - m_exp);
+      l = fmaf(f, lds.stats[w][1][qi], l);
       t += f * *(const SA_LDS f32x4*)(os + (w * 16 + qi) * D + 4 * (ch ^ qi));
     }
     const int64_t row = (int64_t)b * a.Hq + (int64_t)h * G + g0 + qi;
@@ -321,6 +338,49 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeAr
       }
     }
   }
+}
+
+constexpr int kDecodeWaves = 4;
+
+template <int D>
+__global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeArgs a, int parts,
+                                                                        int groups) {
+  __shared__ AttendLds<D, kDecodeWaves> lds;
+  const int part = blockIdx.x % parts;
+  const int rest = blockIdx.x / parts;
+  const int bh = rest / groups;
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int cnt = min(a.topk, (length_of(a, b) + a.blk - 1) / a.blk);
+  const int per = (cnt + parts - 1) / parts;
+  const int i0 = min(part * per, cnt), i1 = min(i0 + per, cnt);
+  const const_ints list = constant(a.blocks) + (int64_t)bh * a.topk + i0;
+  attend<D, kDecodeWaves>(a, b, h, rest % groups, part, parts, i0, i1, [&](int i) { return list[i]; },
+                          lds);
+}
+
+// Selection and attention in one launch, a workgroup a (sequence, key head, group of
+// queries), where few blocks are taken: three launches and a join of parts take longer
+// than the keys and values themselves.
+constexpr int kFusedWaves = 8;
+constexpr int kFusedUnits = 64;     // 32 keys each: eight rounds of the wavefronts
+constexpr int kFusedBlocks = 2048;  // scores in LDS beside the value tiles
+
+template <int D>
+__global__ __launch_bounds__(64 * kFusedWaves) void decode_fused_kernel(DecodeArgs a, int groups) {
+  extern __shared__ uint64_t keys[];  // [n_blk]
+  __shared__ AttendLds<D, kFusedWaves> lds;
+  __shared__ int32_t list[kFusedUnits / 2];
+  static_assert(sizeof(ChooseLds<D, 64 * kFusedWaves>) <= sizeof(lds.Vs), "sums before the values");
+  const int bh = blockIdx.x / groups, hg = blockIdx.x % groups;
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int n = choose<D, 64 * kFusedWaves>(
+      a, b, h, keys, *(ChooseLds<D, 64 * kFusedWaves>*)lds.Vs, [&](int at, int v) { list[at] = v; });
+  __syncthreads();
+  if (hg == 0)
+    for (int i = threadIdx.x; i < a.topk; i += 64 * kFusedWaves)
+      a.blocks[(int64_t)bh * a.topk + i] = i < n ? list[i] : -1;
+  attend<D, kFusedWaves>(a, b, h, hg, 0, 1, 0, n,
+                         [&](int i) { return __builtin_amdgcn_readfirstlane(list[i]); }, lds);
 }
 
 // A wavefront a row: its parts' sums, in order.  Lane p holds the weight of part p (64 at a
@@ -382,9 +442,14 @@ int head_groups(int Hq, int Hkv) { return (Hq / Hkv + kDecodeGroup - 1) / kDecod
 template <int D>
 hipError_t launch_d(const DecodeArgs& a, hipStream_t stream) {
   const int64_t rows = (int64_t)a.B * a.Hkv;
-  const int parts = decode_parts(a.B, a.Hq, a.Hkv, a.n_blk, a.topk);
+  const int parts = decode_parts(a.B, a.Hq, a.Hkv, a.n_blk, a.topk, a.blk);
   const int groups = head_groups(a.Hq, a.Hkv);
   const int lds = a.n_blk * 8;
+  if (parts == 0) {
+    hipLaunchKernelGGL(decode_fused_kernel<D>, dim3((unsigned)(rows * groups)), dim3(64 * kFusedWaves),
+                       lds, stream, a, groups);
+    return hipGetLastError();
+  }
   if (lds > 60 * 1024) {
     const hipError_t e = hipFuncSetAttribute((const void*)decode_select_kernel<D>,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -405,9 +470,10 @@ hipError_t launch_d(const DecodeArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk) {
+int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk, int blk) {
   const int64_t rows = (int64_t)B * Hkv * head_groups(Hq, Hkv);
   const int most = topk < n_blk ? topk : n_blk;
+  if ((int64_t)topk * (blk / 32) <= kFusedUnits && n_blk <= kFusedBlocks) return 0;
   const int64_t parts = (1024 + rows - 1) / rows;
   return (int)(parts < most ? parts : most);
 }

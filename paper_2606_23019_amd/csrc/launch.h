@@ -104,8 +104,9 @@ struct DecodeArgs {
   float scale;
 };
 
-// Parts that a row's blocks are walked in, each by a workgroup of its own.
-int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk);
+// Parts that a row's blocks are walked in, each by a workgroup of its own; 0: selection and
+// attention are one launch.
+int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk, int blk);
 
 hipError_t launch_selected_decode(const DecodeArgs& a, hipStream_t stream);
 

@@ -379,8 +379,8 @@ SA_API int sa_bsattn_bwd(const void* dout, const void* q, const void* k, const v
 
 SA_API size_t sa_selected_decode_workspace(int B, int Hq, int Hkv, int cap, int d, int blk, int topk) {
   if (decode_shape(B, Hq, Hkv, cap, d, blk, topk) != SA_OK) return 0;
-  const int parts = sa::decode_parts(B, Hq, Hkv, (int)cdiv(cap, blk), topk);
-  return align_up(parts > 1 ? (size_t)B * Hq * parts * (d + 2) * 4 : 256);
+  const int parts = sa::decode_parts(B, Hq, Hkv, (int)cdiv(cap, blk), topk, blk);
+  return parts > 1 ? align_up((size_t)B * Hq * parts * (d + 2) * 4) : 0;
 }
 
 SA_API int sa_selected_decode(const void* q, const void* k, const void* v, const int64_t* kv_strides,
@@ -389,7 +389,8 @@ SA_API int sa_selected_decode(const void* q, const void* k, const void* v, const
                               int d, int blk, int topk, float scale, void* stream) {
   const int st = decode_shape(B, Hq, Hkv, cap, d, blk, topk);
   if (st != SA_OK) return st;
-  if (!q || !k || !v || !means || !lengths || !out || !lse || !blocks || !workspace)
+  const size_t ws_bytes = sa_selected_decode_workspace(B, Hq, Hkv, cap, d, blk, topk);
+  if (!q || !k || !v || !means || !lengths || !out || !lse || !blocks || (ws_bytes && !workspace))
     return SA_ERR_INVALID_ARG;
   if (!scale_ok(scale)) return SA_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(means, 16) ||
@@ -403,7 +404,7 @@ SA_API int sa_selected_decode(const void* q, const void* k, const void* v, const
                        {means, (size_t)B * Hkv * n_blk * d * 4}, {lengths, (size_t)B * 4}};
   const Span outs[4] = {{out, (size_t)B * Hq * d * 2}, {lse, (size_t)B * Hq * 4},
                         {blocks, (size_t)B * Hkv * topk * 4},
-                        {workspace, sa_selected_decode_workspace(B, Hq, Hkv, cap, d, blk, topk)}};
+                        {workspace, ws_bytes}};
   if (clash(outs, ins)) return SA_ERR_INVALID_ARG;
   sa::DecodeArgs a{q, k, v, means, lengths, out, lse, blocks, (float*)workspace, B, Hq, Hkv, cap, d,
                    blk, n_blk, topk, kv_strides[0], kv_strides[1], kv_strides[2], scale};

@@ -131,11 +131,11 @@ def decode(lib, q=at(0), k=at(1), s=None, means=at(3), lengths=at(4), out=at(5),
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(q=0), INVALID), (dict(means=0), INVALID), (dict(lengths=0), INVALID), (dict(ws=0), INVALID),
+    (dict(q=0), INVALID), (dict(means=0), INVALID), (dict(lengths=0), INVALID), (dict(ws=0, topk=99), INVALID),
     (dict(k=at(1) + 8), INVALID), (dict(Hq=9), INVALID), (dict(topk=0), INVALID), (dict(cap=0), INVALID),
     (dict(d=96), UNSUPPORTED), (dict(blk=16), UNSUPPORTED), (dict(cap=64 * 16385), UNSUPPORTED),
     (dict(s=strides(0, 0, 129)), INVALID), (dict(out=at(0)), INVALID), (dict(blocks=at(5) + 64), INVALID),
-    (dict(ws=at(1) + 256), INVALID), (dict(scale=float("inf")), INVALID),
+    (dict(ws=at(1) + 256, topk=99), INVALID), (dict(scale=float("inf")), INVALID),
 ])
 def test_decode_refuses(lib, kw, code):
     assert decode(lib, **kw) == code
@@ -145,6 +145,8 @@ def test_workspaces_of_refused_sizes_are_zero(lib):
     assert lib.sa_selected_attn_workspace(1, 1, 0, 64, 64, 64) == 0
     assert lib.sa_bsattn_bwd_workspace(2, 1, 64, 64, 64, 64, 3) == 0
     assert lib.sa_selected_decode_workspace(1, 3, 2, 64, 64, 64, 1) == 0
+    assert lib.sa_selected_decode_workspace(1, 2, 2, 64, 64, 64, 1) == 0  # needs none
+    assert lib.sa_selected_decode_workspace(1, 2, 2, 10000, 64, 64, 99) > 0
     assert lib.sa_bsattn_bwd_workspace(1, 1, 64, 64, 64, 64, 1) % 256 == 0
 
 
