@@ -25,6 +25,7 @@
 
 #include "attn_tiles.h"
 #include "launch.h"
+#include "topk_border.h"
 
 namespace sa {
 
@@ -146,6 +147,7 @@ __global__ __launch_bounds__(256) void bwd_prep_kernel(BwdArgs a, PrepGrid grid)
 constexpr int kPlaces = 512;            // two workgroups on each of 256 compute units
 constexpr int kFront = 2 * kPlaces;     // parts at most: c > limit makes less than c / limit + 1
 constexpr int kLeast = 2;               // shortest part, in list entries
+constexpr int kStaged = 8192;           // counts that the plan keeps in LDS
 constexpr int kClasses = 4;             // of list length: over 2, 1 and 1 / 2 of the mean, others
 
 struct PlanSide {
@@ -160,25 +162,29 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
                                                         int heads) {
   __shared__ int sums[1024];
   __shared__ int class_count[kClasses];
+  __shared__ int staged[kStaged];  // the counts, where they fit
   const PlanSide& o = blockIdx.y ? columns : rows;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int own = mask_heads * o.n_own;   // counts
   int t = 0;
-  for (int i = tid; i < own; i += 1024) t += o.counts[i];
-  sums[tid] = t;
-  __syncthreads();
-  for (int s = 512; s > 0; s >>= 1) {
-    if (tid < s) sums[tid] += sums[tid + s];
-    __syncthreads();
+  for (int i = tid; i < own; i += 1024) {
+    const int c = o.counts[i];
+    if (own <= kStaged) staged[i] = c;
+    t += c;
   }
-  // a count of list entries fits 31 bits where its lists fit in memory; the batch may not
-  const int64_t total = (int64_t)sums[0] * (heads / mask_heads);
-  const int limit = (int)max((int64_t)o.least, (total + kPlaces - 1) / kPlaces);
-  const int mean = max(1, sums[0] / own);
+  const int* counts = own <= kStaged ? staged : o.counts;
+  t = wave_sum(t);
+  if (lane == 0) sums[wave] = t;
   __syncthreads();
+  t = lane < 16 ? sums[lane] : 0;
+  t = wave_sum(t);
+  __syncthreads();
+  const int64_t total = (int64_t)t * (heads / mask_heads);
+  const int limit = (int)max((int64_t)o.least, (total + kPlaces - 1) / kPlaces);
+  const int mean = max(1, t / own);
   auto count_of = [&](int item) {
     const int bh = item / o.n_own;
-    return o.counts[(int64_t)(bh % mask_heads) * o.n_own + (item - bh * o.n_own)];
+    return counts[(int64_t)(bh % mask_heads) * o.n_own + (item - bh * o.n_own)];
   };
   if (blockIdx.x == kXcds) {  // the parts, in the order of the items
     if (o.front == 0) {
@@ -195,15 +201,22 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
         ++splits;
       }
     }
-    sums[tid] = parts | splits << 16;  // both at most kFront
-    __syncthreads();
-    for (int s = 1; s < 1024; s <<= 1) {
-      const int x = tid >= s ? sums[tid - s] : 0;
-      __syncthreads();
-      sums[tid] += x;
-      __syncthreads();
+    const int mine_sum = parts | splits << 16;  // both at most kFront
+    int before = mine_sum;  // inclusive, inside the wavefront
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int x = __shfl_up(before, s, 64);
+      before += lane >= s ? x : 0;
     }
-    int slot = (sums[tid] & 0xffff) - parts, at = (sums[tid] >> 16) - splits;
+    if (lane == 63) sums[wave] = before;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < 16; ++w) {
+      before += w < wave ? sums[w] : 0;
+      all += sums[w];
+    }
+    before -= mine_sum;
+    int slot = before & 0xffff, at = before >> 16;
     for (int i = i0; i < i1; ++i) {
       const int c = count_of(i);
       if (c <= limit) continue;
@@ -214,9 +227,9 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
         o.table[slot] = make_int4(i, first, (int)((int64_t)(p + 1) * c / n) - first, slot);
       }
     }
-    const int used = sums[1023] & 0xffff;
+    const int used = all & 0xffff;
     for (int i = used + tid; i < o.front; i += 1024) o.table[i] = make_int4(0, 0, -1, -1);
-    if (tid == 0) *o.n_splits = sums[1023] >> 16;
+    if (tid == 0) *o.n_splits = all >> 16;
     return;
   }
   // sequence x: a wavefront a class, which finds its members' number and then their places
@@ -266,9 +279,10 @@ struct Item {
   const_ints list;
 };
 
-__device__ __forceinline__ Item item_of(const BwdArgs& a, const BwdSide& l, int n_own, int n_walked) {
+__device__ __forceinline__ Item item_of(const BwdArgs& a, const BwdSide& l, int place, int n_own,
+                                        int n_walked) {
   typedef SA_CONST i32x4* Entries;
-  const i32x4 e = *((Entries)(uintptr_t)l.table + blockIdx.x);
+  const i32x4 e = *((Entries)(uintptr_t)l.table + place);
   Item r;
   r.bh = e.x / n_own;
   r.block = e.x - (int)r.bh * n_own;
@@ -289,27 +303,35 @@ __device__ __forceinline__ void store_part(const f32x16 (&o)[D / 32], float* at,
           f32x4{o[dg][i], o[dg][i + 1], o[dg][i + 2], o[dg][i + 3]};
 }
 
-// Joins the parts of split items: a wavefront 32 rows x 32 columns of one of them.
+// Joins the parts of cut lists: a wavefront 32 rows x 32 columns of one result of one item.
+struct JoinSide {
+  BwdSide side;
+  int n_own, blk, results, blocks;  // results: dQ alone, or dK and dV; blocks of the launch
+};
+
 template <int D>
-__global__ __launch_bounds__(256) void bwd_join_kernel(BwdArgs a, BwdSide l, int n_own, int blk,
-                                                       int results) {
+__global__ __launch_bounds__(256) void bwd_join_kernel(BwdArgs a, JoinSide rows, JoinSide columns) {
+  const bool first = (int)blockIdx.x < rows.blocks;
+  const JoinSide& o = first ? rows : columns;
+  const BwdSide& l = o.side;
+  const int blk = o.blk, results = o.results, n_own = o.n_own;
   const int per = blk / 32 * (D / 32) * results;  // wavefronts an item
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t w = (int64_t)(blockIdx.x - (first ? 0 : rows.blocks)) * 4 + (threadIdx.x >> 6);
   const int at = (int)(w / per);
   if (at >= *l.n_splits) return;
   const int4 e = l.splits[at];
   const int unit = (int)(w - (int64_t)at * per);
   const int dg = unit % (D / 32), rest = unit / (D / 32);
-  const int which = rest % results, rows = rest / results;  // result, group of 32 rows
+  const int which = rest % results, group = rest / results;  // result, 32 rows
   const int lane = threadIdx.x & 63;
-  const float* from = a.parts + ((int64_t)e.y * (blk / 32) * results + rows * results + which) * (32 * D) +
+  const float* from = l.parts + ((int64_t)e.y * (blk / 32) * results + group * results + which) * (32 * D) +
                       dg * 1024 + lane * 4;
   f32x4 t[4] = {};
   for (int p = 0; p < e.z; ++p)
 #pragma unroll
     for (int i = 0; i < 4; ++i) t[i] += *(const f32x4*)(from + (int64_t)p * blk * D * results + i * 256);
   const int64_t bh = e.x / n_own;
-  const int row = (e.x - (int)bh * n_own) * blk + rows * 32 + (lane & 31);
+  const int row = (e.x - (int)bh * n_own) * blk + group * 32 + (lane & 31);
   if (row >= a.N) return;
   __bf16* out = (__bf16*)(results == 1 ? a.dq : which ? a.dv : a.dk);
   const float f = which ? 1.f : a.scale;
@@ -319,14 +341,19 @@ __global__ __launch_bounds__(256) void bwd_join_kernel(BwdArgs a, BwdSide l, int
 }
 
 // ---- dQ ----
+template <int D>
+struct DqLds {
+  __attribute__((aligned(1024))) __bf16 tiles[2][2][kWalk * D];  // buffer, K or V
+};
+
 template <int BQ, int D>
-__global__ __launch_bounds__(BQ * 2, 2) void bwd_dq_kernel(BwdArgs a, BwdSide side) {
+__device__ __forceinline__ void bwd_dq(const BwdArgs& a, const BwdSide& side, int place, DqLds<D>& lds) {
   using T = Tile<BQ, kWalk, D>;
-  __shared__ __attribute__((aligned(1024))) __bf16 tiles[2][2][kWalk * D];  // buffer, K or V
+  auto& tiles = lds.tiles;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const Item item = item_of(a, side, a.n_qb, a.n_kb);
+  const Item item = item_of(a, side, place, a.n_qb, a.n_kb);
   if (item.cnt < 0) return;
   const int64_t base = (item.bh / a.H) * a.sb + (item.bh % a.H) * a.sh;
   const __bf16* Kb = (const __bf16*)a.k + base - kCopyShift;
@@ -401,7 +428,7 @@ __global__ __launch_bounds__(BQ * 2, 2) void bwd_dq_kernel(BwdArgs a, BwdSide si
     }
   }
   if (item.slot >= 0) {
-    store_part<D>(dq, a.parts + ((int64_t)item.slot * (BQ / 32) + wave) * (32 * D), lane);
+    store_part<D>(dq, side.parts + ((int64_t)item.slot * (BQ / 32) + wave) * (32 * D), lane);
     return;
   }
   barrier_tiles();  // the tiles are free
@@ -420,17 +447,25 @@ template <int D>
 constexpr int kWalkRows = kVInLds<D> ? 32 : 64;
 
 template <int BK, int D>
-__global__ __launch_bounds__(BK * 2, 2) void bwd_dkv_kernel(BwdArgs a, BwdSide side) {
+struct DkvLds {
+  __attribute__((aligned(1024))) __bf16 tiles[2][2][kWalkRows<D> * D];  // buffer, Q or dO
+  __attribute__((aligned(1024))) __bf16 Vs[kVInLds<D> ? BK * D : 8];
+  __attribute__((aligned(1024))) float rows[2][2][64];  // buffer, -lse or -D
+};
+
+template <int BK, int D>
+__device__ __forceinline__ void bwd_dkv(const BwdArgs& a, const BwdSide& side, int place,
+                                        DkvLds<BK, D>& lds) {
   constexpr int W = kWalkRows<D>;
   using T = Tile<BK, W, D>;
   using TV = Tile<BK, BK, D>;
-  __shared__ __attribute__((aligned(1024))) __bf16 tiles[2][2][W * D];  // buffer, Q or dO
-  __shared__ __attribute__((aligned(1024))) __bf16 Vs[kVInLds<D> ? BK * D : 8];
-  __shared__ __attribute__((aligned(1024))) float rows[2][2][64];  // buffer, -lse or -D
+  auto& tiles = lds.tiles;
+  auto& Vs = lds.Vs;
+  auto& rows = lds.rows;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, l32 = lane & 31;
-  const Item item = item_of(a, side, a.n_kb, a.n_qb);
+  const Item item = item_of(a, side, place, a.n_kb, a.n_qb);
   if (item.cnt < 0) return;
   const int64_t base = (item.bh / a.H) * a.sb + (item.bh % a.H) * a.sh;
   const __bf16* Qb = (const __bf16*)a.q + base - kCopyShift;
@@ -526,19 +561,45 @@ __global__ __launch_bounds__(BK * 2, 2) void bwd_dkv_kernel(BwdArgs a, BwdSide s
     }
   }
   if (item.slot >= 0) {
-    float* at = a.parts + ((int64_t)item.slot * (BK / 32) + wave) * (2 * 32 * D);
+    float* at = side.parts + ((int64_t)item.slot * (BK / 32) + wave) * (2 * 32 * D);
     store_part<D>(dk, at, lane);
     store_part<D>(dv, at + 32 * D, lane);
     return;
   }
   barrier_tiles();
   char* slice = (char*)tiles + wave * (32 * D * 2);
-  static_assert(sizeof(tiles) >= BK * D * 2, "the tiles hold the results");
+  static_assert(sizeof(lds.tiles) >= BK * D * 2, "the tiles hold the results");
   store_rows_staged<D, __bf16>(dk, a.scale, slice, (__bf16*)a.dk + base + (int64_t)row0 * a.sn, a.sn,
                                a.N - row0, lane);
   // the wavefront's own LDS reads and writes complete in order
   store_rows_staged<D, __bf16>(dv, 1.f, slice, (__bf16*)a.dv + base + (int64_t)row0 * a.sn, a.sn,
                                a.N - row0, lane);
+}
+
+// Both in one launch where their workgroups are of one size, so that one's last items run
+// beside the other's: key blocks first, which take longer.  BQ or BK of 0: the other alone.
+template <int BQ, int BK, int D>
+union BwdLds {
+  DqLds<D> dq;
+  DkvLds<BK ? BK : BQ, D> dkv;
+};
+
+template <int BQ, int BK, int D>
+__global__ __launch_bounds__((BQ ? BQ : BK) * 2, 2) void bwd_kernel(BwdArgs a, BwdSide rows,
+                                                                   BwdSide columns, int dkv_places) {
+  if constexpr (BQ == 0) {
+    __shared__ DkvLds<BK, D> lds;
+    bwd_dkv<BK, D>(a, columns, blockIdx.x, lds);
+  } else if constexpr (BK == 0) {
+    __shared__ DqLds<D> lds;
+    bwd_dq<BQ, D>(a, rows, blockIdx.x, lds);
+  } else {
+    __shared__ BwdLds<BQ, BK, D> lds;
+    if ((int)blockIdx.x < dkv_places)
+      bwd_dkv<BK, D>(a, columns, blockIdx.x, lds.dkv);
+    else
+      bwd_dq<BQ, D>(a, rows, blockIdx.x - dkv_places, lds.dq);
+  }
 }
 
 // Front entries of a table: parts at most, none where no list can be cut.
@@ -567,26 +628,32 @@ hipError_t launch_d(const BwdArgs& a, const BwdWork& w, char* ws, hipStream_t st
   const PlanSide columns = side(w.columns, a.column_counts, a.n_kb);
   hipLaunchKernelGGL(bwd_plan_kernel, dim3(kXcds + 1, 2), dim3(1024), 0, stream, rows, columns,
                      a.mask_heads, (int)bh);
-  const BwdSide r{a.row_lists, rows.table, rows.splits, rows.n_splits};
-  const BwdSide c{a.column_lists, columns.table, columns.splits, columns.n_splits};
-  const unsigned dq_grid = (unsigned)(rows.front + items_padded(rows.n_items));
-  const unsigned dkv_grid = (unsigned)(columns.front + items_padded(columns.n_items));
-  if (a.blk_q == 128)
-    hipLaunchKernelGGL((bwd_dq_kernel<128, D>), dim3(dq_grid), dim3(256), 0, stream, a, r);
-  else
-    hipLaunchKernelGGL((bwd_dq_kernel<64, D>), dim3(dq_grid), dim3(128), 0, stream, a, r);
+  const BwdSide r{a.row_lists, rows.table, rows.splits, rows.n_splits, (float*)(ws + w.rows.parts)};
+  const BwdSide c{a.column_lists, columns.table, columns.splits, columns.n_splits,
+                  (float*)(ws + w.columns.parts)};
+  const int dq_grid = (int)(rows.front + items_padded(rows.n_items));
+  const int dkv_grid = (int)(columns.front + items_padded(columns.n_items));
+  if (a.blk_q == a.blk_k) {
+    const dim3 grid2((unsigned)(dq_grid + dkv_grid));
+    if (a.blk_q == 128)
+      hipLaunchKernelGGL((bwd_kernel<128, 128, D>), grid2, dim3(256), 0, stream, a, r, c, dkv_grid);
+    else
+      hipLaunchKernelGGL((bwd_kernel<64, 64, D>), grid2, dim3(128), 0, stream, a, r, c, dkv_grid);
+  } else if (a.blk_q == 128) {
+    hipLaunchKernelGGL((bwd_kernel<0, 64, D>), dim3(dkv_grid), dim3(128), 0, stream, a, r, c, dkv_grid);
+    hipLaunchKernelGGL((bwd_kernel<128, 0, D>), dim3(dq_grid), dim3(256), 0, stream, a, r, c, 0);
+  } else {
+    hipLaunchKernelGGL((bwd_kernel<0, 128, D>), dim3(dkv_grid), dim3(256), 0, stream, a, r, c, dkv_grid);
+    hipLaunchKernelGGL((bwd_kernel<64, 0, D>), dim3(dq_grid), dim3(128), 0, stream, a, r, c, 0);
+  }
   auto join = [&](const BwdSide& x, const PlanSide& p, int blk, int results) {
-    if (p.front == 0) return;
     const int64_t waves = (int64_t)(p.front / 2) * (blk / 32) * (D / 32) * results;
-    hipLaunchKernelGGL(bwd_join_kernel<D>, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, a, x,
-                       p.n_own, blk, results);
+    return JoinSide{x, p.n_own, blk, results, (int)((waves + 3) / 4)};
   };
-  join(r, rows, a.blk_q, 1);
-  if (a.blk_k == 128)
-    hipLaunchKernelGGL((bwd_dkv_kernel<128, D>), dim3(dkv_grid), dim3(256), 0, stream, a, c);
-  else
-    hipLaunchKernelGGL((bwd_dkv_kernel<64, D>), dim3(dkv_grid), dim3(128), 0, stream, a, c);
-  join(c, columns, a.blk_k, 2);
+  const JoinSide jr = join(r, rows, a.blk_q, 1), jc = join(c, columns, a.blk_k, 2);
+  if (jr.blocks + jc.blocks > 0)
+    hipLaunchKernelGGL(bwd_join_kernel<D>, dim3((unsigned)(jr.blocks + jc.blocks)), dim3(256), 0, stream,
+                       a, jr, jc);
   return hipGetLastError();
 }
 
@@ -616,9 +683,8 @@ BwdWork bwd_work(int B, int H, int mask_heads, int n_qb, int n_kb, int n_pad, in
   w.columns = side(n_kb, n_qb);
   w.nlse = take((size_t)bh * n_pad * 4);
   w.ndelta = take((size_t)bh * n_pad * 4);
-  // the two kernels' parts take turns
-  const size_t dq = (size_t)w.rows.front * blk_q * d * 4, dkv = (size_t)w.columns.front * blk_k * d * 8;
-  w.parts = take(dq > dkv ? dq : dkv);
+  w.rows.parts = take((size_t)w.rows.front * blk_q * d * 4);
+  w.columns.parts = take((size_t)w.columns.front * blk_k * d * 8);
   w.total = at;
   return w;
 }
@@ -634,7 +700,6 @@ hipError_t launch_attention_bwd(const BwdArgs& a, void* workspace, hipStream_t s
   b.column_lists = (int32_t*)(ws + w.columns.lists);
   b.nlse = (float*)(ws + w.nlse);
   b.ndelta = (float*)(ws + w.ndelta);
-  b.parts = (float*)(ws + w.parts);
   return a.d == 128 ? launch_d<128>(b, w, ws, stream) : launch_d<64>(b, w, ws, stream);
 }
 

@@ -135,7 +135,6 @@ struct BwdArgs {
   int32_t* column_lists;   // [mask_heads][n_kb][n_qb]
   float* nlse;             // [B H][n_pad]
   float* ndelta;
-  float* parts;
 };
 
 // Lists that a kernel walks, and the plan of its workgroups.
@@ -144,17 +143,18 @@ struct BwdSide {
   const int4* table;
   const int4* splits;
   const int32_t* n_splits;
+  float* parts;  // sums of the parts, a slot each
 };
 
 // Offsets in the workspace; `front`: entries of a table for parts of cut lists.
 struct BwdSideWork {
-  size_t counts, lists, table, splits, n_splits;
+  size_t counts, lists, table, splits, n_splits, parts;
   int front;
 };
 
 struct BwdWork {
   BwdSideWork rows, columns;
-  size_t nlse, ndelta, parts, total;
+  size_t nlse, ndelta, total;
 };
 
 BwdWork bwd_work(int B, int H, int mask_heads, int n_qb, int n_kb, int n_pad, int d, int blk_q,

@@ -136,13 +136,23 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
   for (int row = wave; row < n_rows; row += waves) {
     const int64_t at = ((int64_t)bh * a.n_qb + u0 + row);
     const int64_t shared = ((int64_t)h * a.n_qb + u0 + row);
+    // mask words, 64 at a time: lane l loads word w0 + l, and all take word i from lane i
     const uint64_t* cand =
         a.candidates ? a.candidates + (a.cand_per_batch ? at : shared) * words : nullptr;
     const uint64_t* keep = a.keep ? a.keep + (a.keep_per_batch ? at : shared) * words : nullptr;
+    auto words_from = [&](const uint64_t* p, int w0) { return p && w0 + lane < words ? p[w0 + lane] : 0; };
+    auto word_of = [](uint64_t mine, int i) {
+      return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, i) |
+             (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), i) << 32;
+    };
     uint64_t* keys = keys_all + row * n_pad;
+    uint64_t kept = words_from(keep, 0);
     if (cand)
-      for (int w = 0; w < words; ++w)
-        if (64 * w + lane < a.n_kb && !((cand[w] >> lane) & 1ull)) keys[64 * w + lane] = 0;
+      for (int w0 = 0; w0 < words; w0 += 64) {
+        const uint64_t mine = words_from(cand, w0);
+        for (int w = w0; w < min(w0 + 64, words); ++w)
+          if (64 * w + lane < a.n_kb && !((word_of(mine, w - w0) >> lane) & 1ull)) keys[64 * w + lane] = 0;
+      }
     Border edge;
     if (words <= 4)
       edge = border_of<4>(keys, a.n_kb, a.topk, lane);
@@ -164,8 +174,9 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
         edge.ties = max(0, edge.ties - (int)__popcll(same));
       }
       if (keep) {
+        if (w > 0 && w % 64 == 0) kept = words_from(keep, w);
         const int real = a.n_kb - 64 * w;
-        word |= keep[w] & (real < 64 ? (1ull << real) - 1ull : ~0ull);
+        word |= word_of(kept, w % 64) & (real < 64 ? (1ull << real) - 1ull : ~0ull);
       }
       if (lane == 0) a.bits[at * words + w] = word;
       if (a.counts && ((word >> lane) & 1ull))

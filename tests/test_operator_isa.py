@@ -34,15 +34,19 @@ def test_no_spills_or_scratch(source, texts):
 
 def test_only_tile_copies_inside_the_gradients_loops(texts):
     seen = 0
-    for m in re.finditer(r"^(_ZN2sa\S+bwd_d(?:q|kv)_\S*kernel\S+):.*?^\.Lfunc_end", texts["attn_bwd.hip"],
+    for m in re.finditer(r"^(_ZN2sa\S+10bwd_kernel\S+):.*?^\.Lfunc_end", texts["attn_bwd.hip"],
                          re.M | re.S):
         lines = m.group(0).split("\n")
-        marked = [i for i, l in enumerate(lines) if "in Loop:" in l or "Loop Header" in l]
-        assert marked, m.group(1)
-        lo, hi = min(marked), max(marked) + 1
-        while hi < len(lines) and not re.match(r"^\.LBB", lines[hi]):
-            hi += 1
-        used = {l.split()[0] for l in lines[lo:hi] if re.match(r"^\s+(global_|buffer_|scratch_|flat_)", l)}
-        assert used <= {"global_load_lds_dwordx4", "global_load_lds_dword"}, (m.group(1), used)
+        starts = [i for i, l in enumerate(lines) if re.match(r"^(\.LBB|; %bb)", l)] + [len(lines)]
+        loops = 0
+        for i, j in zip(starts, starts[1:]):
+            # a block's comments say whether it is part of a loop; tile loops have matrix products
+            head = lines[i:i + 3]
+            if not any("Loop" in l for l in head if l.startswith((".LBB", "; %bb")) or ";" in l[:45]):
+                continue
+            loops += any("v_mfma" in l for l in lines[i:j])
+            used = {l.split()[0] for l in lines[i:j] if re.match(r"^\s+(global_|buffer_|scratch_|flat_)", l)}
+            assert used <= {"global_load_lds_dwordx4", "global_load_lds_dword"}, (m.group(1), used)
+        assert loops, m.group(1)
         seen += 1
-    assert seen == 8  # two kernels, two block sizes, two head dims
+    assert seen == 12  # both in one of either block size, each alone of either, two head dims
