@@ -143,7 +143,10 @@ __global__ __launch_bounds__(256) void bwd_prep_kernel(BwdArgs a, PrepGrid grid)
 //   - the others follow in the XCD layout of the forward kernel's schedule (heads in index
 //     order), inside every XCD's sequence the longest first by coarse classes, so that
 //     long lists do not start last and neighbours still share tiles in L2.
-// Places that stay empty have entries < 0.
+// Places that stay empty have entries < 0.  Measured, 2 x 10 heads x 4000 tokens (d = 64,
+// blocks of 64) and 12 x 16000 (64 x 128), us: two classes 127 and 875, four 117 and 822,
+// sixteen 120 and 795 (12 x 32760: 2872, 2845, 2816-2880); limits of half the size 12 x
+// 8000 224 -> 276.
 constexpr int kPlaces = 512;            // two workgroups on each of 256 compute units
 constexpr int kFront = 2 * kPlaces;     // parts at most: c > limit makes less than c / limit + 1
 constexpr int kLeast = 2;               // shortest part, in list entries
@@ -270,7 +273,12 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
     seq[x + kXcds * j] = make_int4(0, 0, -1, -1);
 }
 
-constexpr int kWalk = 64;  // rows of a walked tile
+// Rows of a walked tile of the query kernel.  Workgroups of two wavefronts take half at
+// d = 128, where that puts three of them on a compute unit instead of two (12 heads x
+// 16000 tokens, blocks of 64: 1011 -> 858 us); at d = 64 four of them fit with whole
+// tiles, and halves cost 3-11 %.
+template <int BQ, int D>
+constexpr int kWalk = BQ == 64 && D == 128 ? 32 : 64;
 
 // A workgroup's part of an item: `own` block of 32 kWaves rows, its list's entries.
 struct Item {
@@ -341,14 +349,15 @@ __global__ __launch_bounds__(256) void bwd_join_kernel(BwdArgs a, JoinSide rows,
 }
 
 // ---- dQ ----
-template <int D>
+template <int BQ, int D>
 struct DqLds {
-  __attribute__((aligned(1024))) __bf16 tiles[2][2][kWalk * D];  // buffer, K or V
+  __attribute__((aligned(1024))) __bf16 tiles[2][2][kWalk<BQ, D> * D];  // buffer, K or V
 };
 
 template <int BQ, int D>
-__device__ __forceinline__ void bwd_dq(const BwdArgs& a, const BwdSide& side, int place, DqLds<D>& lds) {
-  using T = Tile<BQ, kWalk, D>;
+__device__ __forceinline__ void bwd_dq(const BwdArgs& a, const BwdSide& side, int place, DqLds<BQ, D>& lds) {
+  constexpr int W = kWalk<BQ, D>;
+  using T = Tile<BQ, W, D>;
   auto& tiles = lds.tiles;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -358,19 +367,21 @@ __device__ __forceinline__ void bwd_dq(const BwdArgs& a, const BwdSide& side, in
   const int64_t base = (item.bh / a.H) * a.sb + (item.bh % a.H) * a.sh;
   const __bf16* Kb = (const __bf16*)a.k + base - kCopyShift;
   const __bf16* Vb = (const __bf16*)a.v + base - kCopyShift;
-  // tiles of kWalk keys: blk_k / kWalk a block, less one where the last block of all ends
-  // in its first half
-  const int shift = a.blk_k == 128 ? 1 : 0;
+  const int per = a.blk_k / W;  // tiles of a block: 1, 2 or 4
+  const int shift = per == 4 ? 2 : per - 1;
   auto block_at = [&](int i) { return min(max(item.list[i], 0), a.n_kb - 1); };
-  int n_tiles = item.cnt << shift;
-  if (shift && item.cnt > 0 && block_at(item.cnt - 1) * a.blk_k + kWalk >= a.N) --n_tiles;
-  auto key_of = [&](int t) { return block_at(t >> shift) * a.blk_k + (shift ? (t & 1) * kWalk : 0); };
+  int n_tiles = 0;
+  if (item.cnt > 0) {  // the last block of all may end early
+    const int left = min(a.blk_k, a.N - block_at(item.cnt - 1) * a.blk_k);
+    n_tiles = ((item.cnt - 1) << shift) + (left + W - 1) / W;
+  }
+  auto key_of = [&](int t) { return block_at(t >> shift) * a.blk_k + (t & (per - 1)) * W; };
   CopyPlan<T, D> cp;
   cp.init(wave, lane, a.sn);
   auto copy = [&](int t) {
     const int key0 = key_of(t);
-    issue_tile_copy<T, kWalk, D>(tiles[t & 1][0], Kb, key0, a.N, a.sn, wave, lane, cp);
-    issue_tile_copy<T, kWalk, D>(tiles[t & 1][1], Vb, key0, a.N, a.sn, wave, lane, cp);
+    issue_tile_copy<T, W, D>(tiles[t & 1][0], Kb, key0, a.N, a.sn, wave, lane, cp);
+    issue_tile_copy<T, W, D>(tiles[t & 1][1], Vb, key0, a.N, a.sn, wave, lane, cp);
   };
   if (n_tiles > 0) copy(0);
 
@@ -400,7 +411,7 @@ __device__ __forceinline__ void bwd_dq(const BwdArgs& a, const BwdSide& side, in
     barrier_tiles();  // tile t landed; every wavefront is done with tile t - 1
     if (t + 1 < n_tiles) copy(t + 1);
 #pragma unroll
-    for (int kg = 0; kg < kWalk / 32; ++kg) {
+    for (int kg = 0; kg < W / 32; ++kg) {
       f32x16 s, p;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -412,7 +423,7 @@ __device__ __forceinline__ void bwd_dq(const BwdArgs& a, const BwdSide& side, in
         s = mfma32x32x16(rows_operand<D>(Ks, kg * 32, dc, lane), qf[dc], s);
         p = mfma32x32x16(rows_operand<D>(Vs, kg * 32, dc, lane), gf[dc], p);
       }
-      if (key0 + kWalk > a.N) {
+      if (key0 + W > a.N) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (key0 + kg * 32 + 16 * (i >> 3) + 8 * half + (i & 7) >= a.N) s[i] = -INFINITY;
@@ -580,18 +591,18 @@ __device__ __forceinline__ void bwd_dkv(const BwdArgs& a, const BwdSide& side, i
 // beside the other's: key blocks first, which take longer.  BQ or BK of 0: the other alone.
 template <int BQ, int BK, int D>
 union BwdLds {
-  DqLds<D> dq;
+  DqLds<BQ ? BQ : BK, D> dq;
   DkvLds<BK ? BK : BQ, D> dkv;
 };
 
 template <int BQ, int BK, int D>
-__global__ __launch_bounds__((BQ ? BQ : BK) * 2, 2) void bwd_kernel(BwdArgs a, BwdSide rows,
+__global__ __launch_bounds__((BQ ? BQ : BK) * 2, D == 64 ? 3 : 2) void bwd_kernel(BwdArgs a, BwdSide rows,
                                                                    BwdSide columns, int dkv_places) {
   if constexpr (BQ == 0) {
     __shared__ DkvLds<BK, D> lds;
     bwd_dkv<BK, D>(a, columns, blockIdx.x, lds);
   } else if constexpr (BK == 0) {
-    __shared__ DqLds<D> lds;
+    __shared__ DqLds<BQ, D> lds;
     bwd_dq<BQ, D>(a, rows, blockIdx.x, lds);
   } else {
     __shared__ BwdLds<BQ, BK, D> lds;
