@@ -474,7 +474,7 @@ int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk, int blk) {
   const int64_t rows = (int64_t)B * Hkv * head_groups(Hq, Hkv);
   const int most = topk < n_blk ? topk : n_blk;
   if ((int64_t)topk * (blk / 32) <= kFusedUnits && n_blk <= kFusedBlocks) return 0;
-  const int64_t parts = (1024 + rows - 1) / rows;
+  const int64_t parts = (512 + rows - 1) / rows;
   return (int)(parts < most ? parts : most);
 }
 

@@ -82,6 +82,7 @@ struct SelectArgs {
   uint64_t* bits;
   int32_t* counts;  // with lists, or both null
   int32_t* lists;
+  int32_t* order;   // the attention kernel's order of B H heads' items, or null
   int B, H, n_qb, n_kb, d, topk;
   bool cand_per_batch, keep_per_batch;
 };

@@ -248,7 +248,7 @@ SA_API int sa_block_select(const float* q_means, const float* k_means, const uin
                        {keep, row_words * keep_batches * 8}};
   const Span outs[3] = {{mask_bits, row_words * B * 8}, {counts, rows * 4}, {lists, rows * n_kb * 4}};
   if (clash(outs, ins)) return SA_ERR_INVALID_ARG;
-  sa::SelectArgs a{q_means, k_means, candidates, keep, mask_bits, counts, lists, B, H, n_qb, n_kb, d,
+  sa::SelectArgs a{q_means, k_means, candidates, keep, mask_bits, counts, lists, nullptr, B, H, n_qb, n_kb, d,
                    topk, candidate_batches > 1, keep_batches > 1};
   return status(sa::launch_block_select(a, (hipStream_t)stream));
 }
@@ -294,14 +294,14 @@ SA_API int sa_selected_attn_fwd(const void* q, const void* k, const void* v,
   int32_t* order = (int32_t*)(ws + w.order);
   const int64_t sb = (int64_t)H * N * d, sh = (int64_t)N * d;
   hipError_t e = sa::launch_block_means({q, sb, sh, d, qm, blk_q}, {k, sb, sh, d, km, blk_k}, B, H, N, d, s);
-  if (e == hipSuccess) {
-    sa::SelectArgs a{qm, km, candidates, keep, mask_bits, counts, lists, B, H, n_qb, n_kb, d, topk,
-                     candidate_batches > 1, keep_batches > 1};
-    e = sa::launch_block_select(a, s);
-  }
   // every (batch, head) pair has rows of its own: the attention of B H heads
   const bool reads_mask = sa::attention_reads_mask(1, B * H, n_qb, n_kb, d, blk_q, blk_k);
-  if (e == hipSuccess && !reads_mask) e = sa::launch_schedule(counts, 1, B * H, n_qb, order, s);
+  if (e == hipSuccess) {
+    sa::SelectArgs a{qm, km, candidates, keep, mask_bits, reads_mask ? nullptr : counts,
+                     reads_mask ? nullptr : lists, reads_mask ? nullptr : order, B, H, n_qb, n_kb, d,
+                     topk, candidate_batches > 1, keep_batches > 1};
+    e = sa::launch_block_select(a, s);
+  }
   if (e == hipSuccess) {
     sa::AttnArgs a{q, k, v, counts, lists, order, out, lse, 1, B * H, N, d, blk_q, blk_k,
                    n_qb, n_kb, scale, (int64_t)B * H * N * d, sh, d};

@@ -101,6 +101,17 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
   const int u0 = (blockIdx.x - bh * groups) * rows;
   const int n_rows = min(rows, a.n_qb - u0);
   const int l16 = lane & 15, g = lane >> 4;
+  // Rows of a selection are of nearly one length, so the attention takes them in the
+  // XCD layout with the heads in index order, with nothing to sort: a share of the
+  // places here instead of the schedule's two launches.
+  if (a.order) {
+    const int64_t items = (int64_t)a.B * a.H * a.n_qb;
+    for (int64_t p = (int64_t)blockIdx.x * THREADS + threadIdx.x; p < items; p += (int64_t)gridDim.x * THREADS) {
+      int u;
+      const int unit = xcd_slice(p, a.B * a.H, a.n_qb, &u);
+      a.order[p] = unit * a.n_qb + u;
+    }
+  }
 
   const float* qrow = a.qm + ((int64_t)bh * a.n_qb + u0 + min(l16, n_rows - 1)) * D + 4 * g;
   const float* kmat = a.km + (int64_t)bh * a.n_kb * D + 4 * g;
