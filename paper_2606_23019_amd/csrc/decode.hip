@@ -8,8 +8,8 @@
 //   out, lse = softmax attention of the group's G queries over the tokens < L of the
 //              chosen blocks.
 //
-// One launch where few blocks are taken (decode_fused_kernel), else two or three:
-// decode_select_kernel writes the chosen blocks in ascending
+// One launch where few blocks are taken (decode_fused_kernel), else two to four:
+// decode_score_kernel scores long tables, decode_select_kernel writes the chosen blocks in ascending
 // order, decode_attn_kernel walks them in `parts` runs, decode_merge_kernel puts the
 // runs together where there is more than one.
 //
@@ -34,30 +34,21 @@ __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) {
   return min(max(a.lengths[b], 0), a.cap);
 }
 
-// ---- selection: a workgroup a (sequence, key head) ----
-// Eight lanes take a block's mean, so a wavefront scores eight blocks at a time, two
-// times over to have enough loads in flight.
+// ---- selection ----
 template <int D, int THREADS>
 struct ChooseLds {
   double qparts[THREADS / D][D];
   double qsum[D];
+  int counts[2][THREADS / 64];
 };
 
-// The chosen blocks of (b, h), in ascending order, to each of `put`'s calls (place, block):
-// places below the returned number.  Every thread of the workgroup calls this; wavefront 0
-// does the choosing, so what it puts into LDS needs a barrier.
-template <int D, int THREADS, typename Put>
-__device__ __forceinline__ int choose(const DecodeArgs& a, int b, int h, uint64_t* keys,
-                                      ChooseLds<D, THREADS>& lds, Put put) {
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// Ordered keys of the scores of blocks v0 .. v1 - 1 of (b, h), to keys[v].  Eight lanes
+// take a block's mean, so a wavefront scores eight blocks at a time, two times over to
+// have enough loads in flight.  The whole workgroup calls this.
+template <int D, int THREADS>
+__device__ __forceinline__ void score_blocks(const DecodeArgs& a, int b, int h, int v0, int v1,
+                                             uint64_t* keys, ChooseLds<D, THREADS>& lds) {
   const int G = a.Hq / a.Hkv;
-  const int n = (length_of(a, b) + a.blk - 1) / a.blk;  // blocks with a token
-  const int last = n - 1;
-  if (n <= a.topk) {  // all of them
-    for (int v = threadIdx.x; v < n; v += THREADS) put(v, v);
-    return n;
-  }
   constexpr int P = THREADS / D;  // heads summed side by side
   const int c = threadIdx.x % D, i0 = threadIdx.x / D;
   const __bf16* q = (const __bf16*)a.q + ((int64_t)b * a.Hq + (int64_t)h * G) * D + c;
@@ -72,20 +63,21 @@ __device__ __forceinline__ int choose(const DecodeArgs& a, int b, int h, uint64_
     lds.qsum[c] = sum;
   }
   __syncthreads();
-  const int part = lane & 7;  // columns 4 part + 32 i .. + 3
+  const int part = threadIdx.x & 7;  // columns 4 part + 32 i .. + 3
   double qs[D / 8];
 #pragma unroll
   for (int i = 0; i < D / 8; ++i) qs[i] = lds.qsum[4 * part + 32 * (i / 4) + i % 4];
   const float* means = a.means + ((int64_t)b * a.Hkv + h) * a.n_blk * D + 4 * part;
   constexpr int U = 2;  // blocks in flight a lane
   constexpr int kStep = THREADS / 8;
-  for (int v0 = threadIdx.x >> 3; v0 < last + (int)(threadIdx.x >> 3); v0 += U * kStep) {
+  const int mine = threadIdx.x >> 3;
+  for (int w0 = v0; w0 < v1; w0 += U * kStep) {
     f32x4 x[U][D / 32];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int i = 0; i < D / 32; ++i)
-        x[u][i] = *(const f32x4*)(means + (int64_t)min(v0 + u * kStep, last - 1) * D + 32 * i);
+        x[u][i] = *(const f32x4*)(means + (int64_t)min(w0 + mine + u * kStep, v1 - 1) * D + 32 * i);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       double t = 0.0;
@@ -93,19 +85,38 @@ __device__ __forceinline__ int choose(const DecodeArgs& a, int b, int h, uint64_
       for (int i = 0; i < D / 8; ++i) t = fma((double)x[u][i / 4][i % 4], qs[i], t);
 #pragma unroll
       for (int s = 1; s < 8; s *= 2) t += __shfl_xor(t, s, 64);
-      if (part == 0 && v0 + u * kStep < last) keys[v0 + u * kStep] = order_key(t);
+      if (part == 0 && w0 + mine + u * kStep < v1) keys[w0 + mine + u * kStep] = order_key(t);
     }
   }
-  __syncthreads();
-  if (wave != 0) return a.topk;
+}
+
+// The chosen blocks of a sequence of n blocks, more than topk, from the keys of all but the
+// last: in ascending order to `put`'s calls (place, block).  The whole workgroup calls
+// this; wavefront 0 writes, so what it puts into LDS needs a barrier.  MOST bounds n.
+template <int D, int THREADS, int MOST, typename Put>
+__device__ __forceinline__ void choose(int topk, int n, const uint64_t* keys,
+                                       ChooseLds<D, THREADS>& lds, Put put) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int last = n - 1;
   const int words = (last + 63) / 64;
+  constexpr int kWaves = THREADS / 64;
+  constexpr int kEach = MOST / 64 / kWaves;  // words a wavefront of the longest row
+  // One wavefront alone where its registers hold the row: a step of all of them takes a
+  // barrier (60000 tokens, blocks of 64: 23.7 and 26.4 us a call; 135000: 53.7 with the
+  // keys of one wavefront in LDS, 37.9).
   Border edge;
+  if (words > 20) {
+    if (kEach <= 4 || words <= 4 * kWaves)
+      edge = group_border<4, kWaves>(keys, last, topk - 1, wave, lane, lds.counts);
+    else
+      edge = group_border<kEach <= 4 ? 4 : kEach, kWaves>(keys, last, topk - 1, wave, lane, lds.counts);
+  }
+  if (wave != 0) return;
   if (words <= 4)
-    edge = border_of<4>(keys, last, a.topk - 1, lane);
+    edge = border_of<4>(keys, last, topk - 1, lane);
   else if (words <= 20)
-    edge = border_of<20>(keys, last, a.topk - 1, lane);
-  else
-    edge = border_of_long(keys, last, a.topk - 1, lane);
+    edge = border_of<20>(keys, last, topk - 1, lane);
   const uint64_t below = (1ull << lane) - 1ull;
   int done = 0;
   for (int w = 0; w < words; ++w) {
@@ -121,20 +132,46 @@ __device__ __forceinline__ int choose(const DecodeArgs& a, int b, int h, uint64_
     done += __popcll(word);
   }
   if (lane == 0) put(done, last);
-  return a.topk;
 }
 
+// Scores of a run of kScoreRun blocks of one (sequence, key head), where a table is long:
+// one workgroup a row would read them all through one compute unit.
+constexpr int kScoreThreads = 512;
+constexpr int kScoreRun = 256;
+
+template <int D>
+__global__ __launch_bounds__(kScoreThreads) void decode_score_kernel(DecodeArgs a, int runs) {
+  __shared__ ChooseLds<D, kScoreThreads> lds;
+  const int bh = blockIdx.x / runs;
+  const int b = bh / a.Hkv;
+  const int n = (length_of(a, b) + a.blk - 1) / a.blk;
+  const int v0 = (int)(blockIdx.x - bh * runs) * kScoreRun, v1 = min(v0 + kScoreRun, n - 1);
+  if (n <= a.topk || v0 >= v1) return;
+  score_blocks<D, kScoreThreads>(a, b, bh - b * a.Hkv, v0, v1, a.keys + (int64_t)bh * a.n_blk, lds);
+}
+
+// A workgroup a (sequence, key head); the scores are its own or decode_score_kernel's.
 constexpr int kDecodeSelectThreads = 1024;
 
 template <int D>
 __global__ __launch_bounds__(kDecodeSelectThreads) void decode_select_kernel(DecodeArgs a) {
-  extern __shared__ uint64_t keys[];  // [n_blk]
+  extern __shared__ uint64_t own_keys[];  // [n_blk], where there are no others
   __shared__ ChooseLds<D, kDecodeSelectThreads> lds;
   const int bh = blockIdx.x;
+  const int b = bh / a.Hkv;
+  const int n = (length_of(a, b) + a.blk - 1) / a.blk;  // blocks with a token
   int32_t* list = a.blocks + (int64_t)bh * a.topk;
-  const int n = choose<D, kDecodeSelectThreads>(a, bh / a.Hkv, bh % a.Hkv, keys, lds,
-                                                [&](int at, int v) { list[at] = v; });
-  for (int i = n + threadIdx.x; i < a.topk; i += kDecodeSelectThreads) list[i] = -1;
+  for (int i = threadIdx.x; i < a.topk; i += kDecodeSelectThreads)
+    if (n <= a.topk) list[i] = i < n ? i : -1;
+  if (n <= a.topk) return;
+  const uint64_t* keys = a.keys + (int64_t)bh * a.n_blk;
+  if (!a.keys) {
+    score_blocks<D, kDecodeSelectThreads>(a, b, bh - b * a.Hkv, 0, n - 1, own_keys, lds);
+    __syncthreads();
+    keys = own_keys;
+  }
+  choose<D, kDecodeSelectThreads, kSelectMaxBlocks>(a.topk, n, keys, lds,
+                                                    [&](int at, int v) { list[at] = v; });
 }
 
 // ---- attention ----
@@ -373,8 +410,17 @@ __global__ __launch_bounds__(64 * kFusedWaves) void decode_fused_kernel(DecodeAr
   static_assert(sizeof(ChooseLds<D, 64 * kFusedWaves>) <= sizeof(lds.Vs), "sums before the values");
   const int bh = blockIdx.x / groups, hg = blockIdx.x % groups;
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;
-  const int n = choose<D, 64 * kFusedWaves>(
-      a, b, h, keys, *(ChooseLds<D, 64 * kFusedWaves>*)lds.Vs, [&](int at, int v) { list[at] = v; });
+  const int blocks = (length_of(a, b) + a.blk - 1) / a.blk;
+  const int n = min(blocks, a.topk);
+  if (blocks <= a.topk) {
+    for (int i = threadIdx.x; i < n; i += 64 * kFusedWaves) list[i] = i;
+  } else {
+    auto& sums = *(ChooseLds<D, 64 * kFusedWaves>*)lds.Vs;
+    score_blocks<D, 64 * kFusedWaves>(a, b, h, 0, blocks - 1, keys, sums);
+    __syncthreads();
+    choose<D, 64 * kFusedWaves, kFusedBlocks>(a.topk, blocks, keys, sums,
+                                              [&](int at, int v) { list[at] = v; });
+  }
   __syncthreads();
   if (hg == 0)
     for (int i = threadIdx.x; i < a.topk; i += 64 * kFusedWaves)
@@ -440,9 +486,8 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(DecodeArgs a, int par
 int head_groups(int Hq, int Hkv) { return (Hq / Hkv + kDecodeGroup - 1) / kDecodeGroup; }
 
 template <int D>
-hipError_t launch_d(const DecodeArgs& a, hipStream_t stream) {
+hipError_t launch_d(const DecodeArgs& a, int parts, hipStream_t stream) {
   const int64_t rows = (int64_t)a.B * a.Hkv;
-  const int parts = decode_parts(a.B, a.Hq, a.Hkv, a.n_blk, a.topk, a.blk);
   const int groups = head_groups(a.Hq, a.Hkv);
   const int lds = a.n_blk * 8;
   if (parts == 0) {
@@ -450,13 +495,13 @@ hipError_t launch_d(const DecodeArgs& a, hipStream_t stream) {
                        lds, stream, a, groups);
     return hipGetLastError();
   }
-  if (lds > 60 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)decode_select_kernel<D>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
+  if (a.keys) {
+    const int runs = (a.n_blk + kScoreRun - 1) / kScoreRun;
+    hipLaunchKernelGGL(decode_score_kernel<D>, dim3((unsigned)(rows * runs)), dim3(kScoreThreads), 0,
+                       stream, a, runs);
   }
-  hipLaunchKernelGGL(decode_select_kernel<D>, dim3((unsigned)rows), dim3(kDecodeSelectThreads), lds,
-                     stream, a);
+  hipLaunchKernelGGL(decode_select_kernel<D>, dim3((unsigned)rows), dim3(kDecodeSelectThreads),
+                     a.keys ? 0 : lds, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(decode_attn_kernel<D>, dim3((unsigned)(rows * groups * parts)),
@@ -470,16 +515,33 @@ hipError_t launch_d(const DecodeArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk, int blk) {
+// Tables of up to this many blocks are scored where they are chosen from; longer ones in a
+// launch of their own, us a call scored in place and apart: 2 rows of 2110 blocks 37.9 and
+// 34.4, 1 row of up to 1563 23.6 and 26.3, 128 rows of up to 1055 116.4 and 117.6.
+constexpr int kScoredInPlace = 2048;
+
+DecodeWork decode_work(int B, int Hq, int Hkv, int n_blk, int topk, int blk, int d) {
+  DecodeWork w{};
   const int64_t rows = (int64_t)B * Hkv * head_groups(Hq, Hkv);
+  if ((int64_t)topk * (blk / 32) <= kFusedUnits && n_blk <= kFusedBlocks) return w;
+  // a round of two workgroups a compute unit (16 x 8 rows of 64 blocks: 118.7 us in rounds
+  // of half the length, 115.8)
   const int most = topk < n_blk ? topk : n_blk;
-  if ((int64_t)topk * (blk / 32) <= kFusedUnits && n_blk <= kFusedBlocks) return 0;
   const int64_t parts = (512 + rows - 1) / rows;
-  return (int)(parts < most ? parts : most);
+  w.parts = (int)(parts < most ? parts : most);
+  if (w.parts > 1) w.total = ((size_t)B * Hq * w.parts * (d + 2) * 4 + 255) / 256 * 256;
+  w.keys = w.total;
+  w.scored = n_blk > kScoredInPlace;
+  if (w.scored) w.total += (size_t)B * Hkv * n_blk * 8;
+  return w;
 }
 
-hipError_t launch_selected_decode(const DecodeArgs& a, hipStream_t stream) {
-  return a.d == 128 ? launch_d<128>(a, stream) : launch_d<64>(a, stream);
+hipError_t launch_selected_decode(const DecodeArgs& args, void* workspace, hipStream_t stream) {
+  DecodeArgs a = args;
+  const DecodeWork w = decode_work(a.B, a.Hq, a.Hkv, a.n_blk, a.topk, a.blk, a.d);
+  a.parts_out = (float*)workspace;
+  a.keys = w.scored ? (uint64_t*)((char*)workspace + w.keys) : nullptr;
+  return a.d == 128 ? launch_d<128>(a, w.parts, stream) : launch_d<64>(a, w.parts, stream);
 }
 
 }  // namespace sa

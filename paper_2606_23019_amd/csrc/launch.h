@@ -99,17 +99,25 @@ struct DecodeArgs {
   void* out;
   float* lse;
   int32_t* blocks;
-  float* parts_out;  // parts > 1: float [B][Hq][parts][d], then [B][Hq][parts][2]
   int B, Hq, Hkv, cap, d, blk, n_blk, topk;
   int64_t sb, sh, sn;  // element strides of k and v: batch, head, token
   float scale;
+  // set by the launcher
+  float* parts_out;  // parts > 1: float [B][Hq][parts][d], then [B][Hq][parts][2]
+  uint64_t* keys;    // scores of long tables [B][Hkv][n_blk], or null
 };
 
-// Parts that a row's blocks are walked in, each by a workgroup of its own; 0: selection and
-// attention are one launch.
-int decode_parts(int B, int Hq, int Hkv, int n_blk, int topk, int blk);
+// Parts that a row's blocks are walked in, each by a workgroup of its own (0: selection and
+// attention are one launch), and the workspace: their sums, then the scores if `scored`.
+struct DecodeWork {
+  int parts;
+  bool scored;
+  size_t keys, total;
+};
 
-hipError_t launch_selected_decode(const DecodeArgs& a, hipStream_t stream);
+DecodeWork decode_work(int B, int Hq, int Hkv, int n_blk, int topk, int blk, int d);
+
+hipError_t launch_selected_decode(const DecodeArgs& a, void* workspace, hipStream_t stream);
 
 struct BwdArgs {
   const void* q;

@@ -379,8 +379,7 @@ SA_API int sa_bsattn_bwd(const void* dout, const void* q, const void* k, const v
 
 SA_API size_t sa_selected_decode_workspace(int B, int Hq, int Hkv, int cap, int d, int blk, int topk) {
   if (decode_shape(B, Hq, Hkv, cap, d, blk, topk) != SA_OK) return 0;
-  const int parts = sa::decode_parts(B, Hq, Hkv, (int)cdiv(cap, blk), topk, blk);
-  return parts > 1 ? align_up((size_t)B * Hq * parts * (d + 2) * 4) : 0;
+  return sa::decode_work(B, Hq, Hkv, (int)cdiv(cap, blk), topk, blk, d).total;
 }
 
 SA_API int sa_selected_decode(const void* q, const void* k, const void* v, const int64_t* kv_strides,
@@ -406,9 +405,9 @@ SA_API int sa_selected_decode(const void* q, const void* k, const void* v, const
                         {blocks, (size_t)B * Hkv * topk * 4},
                         {workspace, ws_bytes}};
   if (clash(outs, ins)) return SA_ERR_INVALID_ARG;
-  sa::DecodeArgs a{q, k, v, means, lengths, out, lse, blocks, (float*)workspace, B, Hq, Hkv, cap, d,
-                   blk, n_blk, topk, kv_strides[0], kv_strides[1], kv_strides[2], scale};
-  return status(sa::launch_selected_decode(a, (hipStream_t)stream));
+  sa::DecodeArgs a{q, k, v, means, lengths, out, lse, blocks, B, Hq, Hkv, cap, d,
+                   blk, n_blk, topk, kv_strides[0], kv_strides[1], kv_strides[2], scale, nullptr, nullptr};
+  return status(sa::launch_selected_decode(a, workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -154,4 +154,48 @@ __device__ __forceinline__ Border border_of_long(const uint64_t* keys, int n_kb,
       [&](uint32_t u, uint32_t t) { return count([=](uint32_t h, uint32_t l) { return h == u && l >= t; }); });
 }
 
+// The border of one row found by all WAVES wavefronts of a workgroup together, each with
+// the keys of W words in registers: rows of up to 64 W WAVES.  `counts` is LDS of 2 x
+// WAVES numbers; every thread calls this, and all get the border.
+template <int W, int WAVES>
+__device__ __forceinline__ Border group_border(const uint64_t* keys, int n_kb, int topk, int wave,
+                                               int lane, int (*counts)[WAVES]) {
+  uint32_t hi[W], lo[W];
+  int n = 0;
+  uint32_t most = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const int v = 64 * (w * WAVES + wave) + lane;
+    const uint64_t key = v < n_kb ? keys[v] : 0;
+    hi[w] = (uint32_t)(key >> 32);
+    lo[w] = (uint32_t)key;
+    n += key != 0;
+    most = max(most, hi[w]);
+  }
+  int turn = 0;  // the numbers of one call are read while those of the next are written
+  auto gather = [&](int mine) {
+    if (lane == 0) counts[turn][wave] = mine;
+    __syncthreads();
+    const int other = lane < WAVES ? counts[turn][lane] : 0;
+    turn ^= 1;
+    return other;
+  };
+  n = wave_sum(gather(wave_sum(n)));
+  most = wave_max((uint32_t)gather((int)wave_max(most)));
+  return find_border<true>(
+      n, topk, most,
+      [&](uint32_t t) {
+        int c = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) c += hi[w] >= t;
+        return wave_sum(gather(wave_sum(c)));
+      },
+      [&](uint32_t h, uint32_t t) {
+        int c = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) c += hi[w] == h && lo[w] >= t;
+        return wave_sum(gather(wave_sum(c)));
+      });
+}
+
 }  // namespace sa

@@ -324,6 +324,8 @@ DECODE = [  # B, Hq, Hkv, cap, d, blk, topk, lengths
     (1, 32, 1, 3000, 64, 128, 7, [2999]),
     (2, 5, 1, 20000, 128, 64, 33, [20000, 15001]),
     (1, 1, 1, 100000, 64, 64, 20, [99999]),
+    (2, 2, 1, 140001, 64, 64, 40, [140001, 70000]),
+    (1, 2, 1, 320001, 64, 64, 40, [320001]),
 ]
 
 
