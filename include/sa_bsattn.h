@@ -350,8 +350,8 @@ SA_API int sa_bsattn_plan_destroy(sa_plan_t plan);
  * int32 [B][N], entries clamped to [0, n_pos), or NULL: token n is at position n
  * (then n_pos >= N).  q_out, k_out: bf16, contiguous [B][H][N][d] or
  * [B][N][H][d] by `layout`, rounded once from fp32.  d in {64, 128}; rot a
- * multiple of 16 up to d; eps >= 0.  Outputs must not overlap inputs or each
- * other.
+ * multiple of 16 up to d; eps >= 0 (0 leaves a row of zeros 0 / 0).  Outputs must
+ * not overlap inputs or each other.
  */
 SA_API int sa_qk_norm_rope(const void* q, const int64_t* q_strides, const void* k,
                            const int64_t* k_strides, const float* wq, const float* wk,
@@ -426,7 +426,7 @@ SA_API int sa_selected_attn_fwd(const void* q, const void* k, const void* v,
  * dq, dk and dv are bf16 in `layout`; lse is [B][H][N].  Query blocks with no set
  * bit get dq = 0, key blocks that no row enables dk = dv = 0.  P and dS are
  * rounded to bf16 for the products, everything else is fp32.  The masks' rows
- * have to have fewer than 2^31 bits in all.
+ * have to have fewer than 2^31 bits in all, and scale is at least 1e-30.
  */
 SA_API size_t sa_bsattn_bwd_workspace(int B, int H, int N, int d, int blk_q, int blk_k,
                                       int mask_batches);

@@ -482,8 +482,9 @@ class Plan:
 # ------------------------------------------------- around the attention ---
 #
 # Tensors may be on any GPU, all on the same one; the work goes to that GPU's
-# current stream, or to ``stream``, which has to be of that GPU.  The checks are
-# written for small calls, which take the host longer than the GPU.
+# current stream, or to ``stream``, which has to be of that GPU and then waits
+# for the current one.  The checks are written for small calls, which take the
+# host longer than the GPU.
 
 _PAIRS = {"interleaved": SA_PAIRS_INTERLEAVED, "halves": SA_PAIRS_HALVES}
 _LAYOUTS = {"bhnd": SA_LAYOUT_BHND, "bnhd": SA_LAYOUT_BNHD}
@@ -560,7 +561,10 @@ def _run(fn, dev, stream, args, made):
     else:
         _need(stream is None or stream.device_index == dev, "stream is not of GPU %d" % dev)
         with torch.cuda.device(dev):
-            st = getattr(load(), fn)(*args, (stream or torch.cuda.current_stream()).cuda_stream)
+            now = torch.cuda.current_stream()
+            if stream is not None and stream != now:
+                stream.wait_stream(now)  # the inputs, and who had the new tensors' memory before
+            st = getattr(load(), fn)(*args, (stream or now).cuda_stream)
             _used_on(stream, *made)
     if st != SA_OK:
         raise SAError(fn, st)

@@ -16,7 +16,7 @@
 
 namespace {
 
-constexpr int kVersion = 300;  // 0.3.0: allocation-free one-shot entry point
+constexpr int kVersion = 400;  // 0.4.0: operators around the attention
 
 struct Dims {
   int n_qb, n_kb, W;

@@ -18,8 +18,14 @@
 // tiles are read from LDS by rows for the first and transposed for the second.  P and
 // dS are rounded to bf16 there, which the products take.
 //
-// bwd_rows_kernel makes what both need of a row: lse in the exponent's unit and D,
+// bwd_prep_kernel makes what both need of a row: lse in the exponent's unit and D,
 // negative, so that the accumulators of S and dP can start from them.
+//
+// Bound: matrix products.  Measured, 12 heads x 32760 tokens (d = 128, blocks of 128, density
+// about 0.13): 2.69-2.75 ms, 7 products at 1.11-1.13 PFLOP/s, the rate of the forward
+// kernel and of a large library product (1.16); the 5 that the formulas need would take 1.87
+// ms at that rate.  2 x 10 heads x 4000 tokens (d = 64, blocks of 64): 110 us, of which 95
+// in the two kernels at 0.79 PFLOP/s: there the exponentials take as long as the products.
 
 #include <math.h>
 
@@ -57,7 +63,7 @@ __device__ __forceinline__ bf16x8 columns_operand(const __bf16* tile, int r0, in
 // s += rows of S times b0, p += rows of P times b1(dc), over all columns.  AHEAD requests
 // the operands of step dc + 1 before the products of step dc: left to itself the compiler
 // reads each just before its use (12 heads x 32760 tokens, d = 128: 2840 -> 2770 us; at d =
-// 64 the registers for it are not there, and for the products by columns not at 128).
+// 64 the registers for it are not there, nor for the products by columns at 128).
 // A wavefront in these products gives way to one in its exponentials and the products
 // after them, which it waits for with more in flight (2740 -> 2670 us; the other way
 // round 2680).
@@ -186,6 +192,7 @@ constexpr int kPlaces = 512;            // two workgroups on each of 256 compute
 constexpr int kFront = 2 * kPlaces;     // parts at most: c > limit makes less than c / limit + 1
 constexpr int kLeast = 2;               // shortest part, in list entries
 constexpr int kStaged = 8192;           // counts that the plan keeps in LDS
+constexpr int kSequence = 4096;         // and places of an XCD's sequence
 constexpr int kClasses = 4;             // of list length: over 2, 1 and 1 / 2 of the mean, others
 
 struct PlanSide {
@@ -201,6 +208,8 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
   __shared__ int sums[1024];
   __shared__ int class_count[kClasses];
   __shared__ int staged[kStaged];  // the counts, where they fit
+  __shared__ int seq_item[kSequence];
+  __shared__ uint8_t seq_class[kSequence];
   const PlanSide& o = blockIdx.y ? columns : rows;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int own = mask_heads * o.n_own;   // counts
@@ -275,18 +284,31 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
   const int units = o.n_items / o.n_own;
   const int len = (o.n_items - x + kXcds - 1) / kXcds;
   int4* seq = o.table + o.front;
-  auto mine = [&](int j, int* item, int* c) {  // whether place j is of the wavefront's class
-    if (j >= len) return false;
+  // the item at place j and its class, kClasses if it is cut; all wavefronts work out the
+  // first kSequence of them, the divisions of the layout once each
+  auto item_at = [&](int j, int* item) {
     int u;
     const int unit = xcd_slice(x + (int64_t)kXcds * j, units, o.n_own, &u);
     *item = unit * o.n_own + u;
-    *c = count_of(*item);
-    const int cls = *c > 2 * mean ? 0 : *c > mean ? 1 : 2 * *c > mean ? 2 : 3;
-    return cls == wave && !(o.front && *c > limit);
+    const int c = count_of(*item);
+    if (o.front && c > limit) return kClasses;
+    return c > 2 * mean ? 0 : c > mean ? 1 : 2 * c > mean ? 2 : 3;
+  };
+  for (int j = tid; j < min(len, kSequence); j += 1024) {
+    int item;
+    seq_class[j] = (uint8_t)item_at(j, &item);
+    seq_item[j] = item;
+  }
+  __syncthreads();
+  auto mine = [&](int j, int* item) {  // whether place j is of the wavefront's class
+    if (j >= len) return false;
+    if (j >= kSequence) return item_at(j, item) == wave;
+    *item = seq_item[j];
+    return seq_class[j] == wave;
   };
   if (wave < kClasses) {
-    int item = 0, c = 0, n = 0;
-    for (int j = lane; j < len + lane; j += 64) n += __popcll(__ballot(mine(j, &item, &c)));
+    int item = 0, n = 0;
+    for (int j = lane; j < len + lane; j += 64) n += __popcll(__ballot(mine(j, &item)));
     if (lane == 0) class_count[wave] = n;
   }
   __syncthreads();
@@ -297,10 +319,10 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
   }
   if (wave < kClasses) {
     for (int j = lane; j < len + lane; j += 64) {
-      int item = 0, c = 0;
-      const bool in = mine(j, &item, &c);
+      int item = 0;
+      const bool in = mine(j, &item);
       const uint64_t on = __ballot(in);
-      if (in) seq[x + kXcds * (base + __popcll(on & ((1ull << lane) - 1ull)))] = make_int4(item, 0, c, -1);
+      if (in) seq[x + kXcds * (base + __popcll(on & ((1ull << lane) - 1ull)))] = make_int4(item, 0, count_of(item), -1);
       base += __popcll(on);
     }
   }

@@ -14,7 +14,12 @@
 // runs together where there is more than one.
 //
 // Bound: HBM bytes of the means and of the chosen blocks' keys and values, which are
-// read once for the whole group; with few rows the latency of the launches.
+// read once for the whole group; with few rows the latency of the launches.  Measured:
+// 16 sequences of up to 135000 tokens, 8 key heads, 64 blocks of 128: 116 us, 4.9 TB/s in
+// all, of which selection 22 (one compute unit a row) and attention 92-98 (5.5-5.8 TB/s;
+// a reduction reads at 5.7); 2 x 12 heads, 16 blocks of 64: 17 us a call, where what one
+// compute unit reads of its row's 0.5 MB bounds it (twice the loads in flight change
+// nothing).
 
 #include <math.h>
 

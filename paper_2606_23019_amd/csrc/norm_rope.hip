@@ -16,6 +16,9 @@
 //
 // Bound: HBM bytes (4 an element forward, 6 backward; some 20 vector instructions
 // for every 8 elements).  Everything is fp32; each output is rounded to bf16 once.
+// Measured: 75600 tokens x 80 heads of 128 in 631 us, 4.97 TB/s (a 2 GiB copy runs at
+// 4.85); gradients of 2 x 32760 tokens x 24 heads in 249 us, 4.93 TB/s.  Eight tokens
+// take 4 us on the GPU and 15 us a call, the host's part.
 
 #include "device_common.h"
 #include "launch.h"
@@ -303,8 +306,8 @@ __global__ __launch_bounds__(256) void norm_rope_dw_kernel(const float* __restri
   }
 }
 
-// Heads a wavefront walks: as many as leave `units` units for the chip, so that a few
-// tokens still spread over it and many share their tables.
+// Heads a wavefront walks: as many as leave `units` units for the chip (eight wavefronts
+// on each SIMD), so that a few tokens still spread over it and many share their tables.
 int heads_per_unit(const RopeArgs& a, int64_t units) {
   const int64_t groups = ((int64_t)a.B * a.N + 512 / a.d - 1) / (512 / a.d);
   int heads = 16;

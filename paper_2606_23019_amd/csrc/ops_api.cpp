@@ -328,7 +328,9 @@ SA_API int sa_bsattn_bwd(const void* dout, const void* q, const void* k, const v
   if (st != SA_OK) return st;
   if (!dout || !q || !k || !v || !out || !lse || !mask_bits || !dq || !dk || !dv || !workspace)
     return SA_ERR_INVALID_ARG;
-  if (!scale_ok(scale) || (mask_batches != 1 && mask_batches != B)) return SA_ERR_INVALID_ARG;
+  // lse / scale has to be a float
+  if (!scale_ok(scale) || scale < 1e-30f || (mask_batches != 1 && mask_batches != B))
+    return SA_ERR_INVALID_ARG;
   if (layout != SA_LAYOUT_BHND && layout != SA_LAYOUT_BNHD) return SA_ERR_INVALID_ARG;
   const void* rows[8] = {dout, q, k, v, out, dq, dk, dv};
   for (const void* p : rows)

@@ -312,6 +312,26 @@ def test_bsattn_bwd(case):
             assert not f64(heads(got[2])[b, h])[~see.any(0)].any()
 
 
+def test_bsattn_bwd_of_many_heads():
+    """More items than the plan holds at once: the heads' results are those of smaller calls, bit
+    for bit (no list is long enough to be cut in either)."""
+    import torch
+    from paper_2606_23019_amd import binding
+    H, N, d, blk = 576, 3840, 64, 64
+    n = N // blk
+    g = gen(9)
+    q, k, v, dout = (randn(g, 1, H, N, d) for _ in range(4))
+    on = np.random.default_rng(9).random((H, n, n)) < 0.08
+    mask = pack(on)
+    out, lse = binding.bsattn_fwd(q, k, v, mask, blk, blk)
+    got = binding.bsattn_bwd(dout, q, k, v, out, lse, mask, blk, blk)
+    for h0 in (0, 300):
+        h = slice(h0, h0 + 276)
+        part = [t[:, h].contiguous() for t in (dout, q, k, v, out)]
+        ref = binding.bsattn_bwd(*part, lse[:, h].contiguous(), mask[h].contiguous(), blk, blk)
+        assert all(torch.equal(a[:, h], b) for a, b in zip(got, ref))
+
+
 # ------------------------------------------------------------ single tokens ---
 
 DECODE = [  # B, Hq, Hkv, cap, d, blk, topk, lengths
@@ -430,15 +450,23 @@ def test_chain_eager_other_stream_and_captured(N, blk):
 
 
 def test_stream_argument():
+    """A call on another stream waits for what made its inputs on the current one."""
     import torch
     from paper_2606_23019_amd import binding
     x, w, tables = chain_inputs(22)
     ref = binding.qk_norm_rope(x[:, :, :3], x[:, :, 3:6], *w, *tables)
     side = torch.cuda.Stream()
+    big = torch.randn((4096, 4096), device="cuda")
     torch.cuda.synchronize()
-    got = binding.qk_norm_rope(x[:, :, :3], x[:, :, 3:6], *w, *tables, stream=side)
-    side.synchronize()
-    assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    for _ in range(3):
+        y = torch.zeros_like(x)
+        for _ in range(8):
+            big = (big @ big).clamp_(-1, 1)  # keeps the current stream busy before y is there
+        y.copy_(x)
+        got = binding.qk_norm_rope(y[:, :, :3], y[:, :, 3:6], *w, *tables, stream=side)
+        y.record_stream(side)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))
 
 
 def test_decode_continues_what_the_prompt_began():

@@ -114,7 +114,7 @@ def bwd(lib, dout=at(0), q=at(1), out=at(4), lse=at(5), m=at(6), mb=1, dq=at(7),
 @pytest.mark.parametrize("kw,code", [
     (dict(dout=0), INVALID), (dict(m=0), INVALID), (dict(q=at(1) + 8), INVALID),
     (dict(lse=at(5) + 2), INVALID), (dict(ws=at(10) + 128), INVALID), (dict(mb=3), INVALID),
-    (dict(mb=0), INVALID), (dict(layout=5), INVALID), (dict(scale=-1.0), INVALID), (dict(N=0), INVALID),
+    (dict(mb=0), INVALID), (dict(layout=5), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=1e-31), INVALID), (dict(N=0), INVALID),
     (dict(d=256), UNSUPPORTED), (dict(bk=256), UNSUPPORTED), (dict(dq=at(0)), INVALID),
     (dict(dv=at(7) + 16), INVALID), (dict(ws=at(5)), INVALID),
     (dict(layout=1, H=1 << 16, d=128), UNSUPPORTED), (dict(N=64 * 65536), UNSUPPORTED),
