@@ -22,9 +22,9 @@
 // negative, so that the accumulators of S and dP can start from them.
 //
 // Bound: matrix products.  Measured, 12 heads x 32760 tokens (d = 128, blocks of 128, density
-// about 0.13): 2.69-2.75 ms, 7 products at 1.11-1.13 PFLOP/s, the rate of the forward
-// kernel and of a large library product (1.16); the 5 that the formulas need would take 1.87
-// ms at that rate.  2 x 10 heads x 4000 tokens (d = 64, blocks of 64): 110 us, of which 95
+// about 0.13): 2.69-2.75 ms, 7 products at 1.10-1.13 PFLOP/s (the forward kernel 1.05-1.1;
+// a large library product 1.16-1.35, depending on the card); the 5 that the formulas need
+// would take 1.6-1.9 ms at the library's rate.  2 x 10 heads x 4000 tokens (d = 64, blocks of 64): 110 us, of which 95
 // in the two kernels at 0.79 PFLOP/s: there the exponentials take as long as the products.
 
 #include <math.h>
