@@ -15,9 +15,9 @@
 //
 // Bound: HBM bytes of the means and of the chosen blocks' keys and values, which are
 // read once for the whole group; with few rows the latency of the launches.  Measured:
-// 16 sequences of up to 135000 tokens, 8 key heads, 64 blocks of 128: 116 us, 4.9 TB/s in
-// all, of which selection 22 (one compute unit a row) and attention 92-98 (5.5-5.8 TB/s;
-// a reduction reads at 5.7); 2 x 12 heads, 16 blocks of 64: 17 us a call, where what one
+// 16 sequences of up to 135000 tokens, 8 key heads, 64 blocks of 128: 104 us, 5.5 TB/s in
+// all, of which selection 22 (one compute unit a row) and attention about 80 (a reduction
+// reads at 5.7 TB/s); 2 x 12 heads, 16 blocks of 64: 17 us a call, where what one
 // compute unit reads of its row's 0.5 MB bounds it (twice the loads in flight change
 // nothing).
 
@@ -222,8 +222,8 @@ struct AttendLds {
 };
 
 // Entries i0 .. i1 - 1 of the list of chosen blocks, block_at(i) for entry i - i0, by the
-// workgroup's WAVES wavefronts; part `part` of `parts`.
-template <int D, int WAVES, typename BlockAt>
+// workgroup's WAVES wavefronts; part `part` of `parts`.  STREAM: read past the caches.
+template <int D, int WAVES, bool STREAM, typename BlockAt>
 __device__ __forceinline__ void attend(const DecodeArgs& a, int b, int h, int hg, int part, int parts,
                                        int i0, int i1, BlockAt block_at, AttendLds<D, WAVES>& lds) {
   constexpr int C = D / 8;        // 16-byte chunks of a row
@@ -258,19 +258,20 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, int b, int h, int hg
   };
   bf16x8 kf[2][D / 32];
   u32x4 vr[kVLoads];
+  auto load = [](const __bf16* p) { return STREAM ? load_stream(p) : *(const u32x4*)p; };
   auto load_k = [&](int key0) {  // rows past the sequence repeat its last one
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const __bf16* row =
           K + (int64_t)min(key0 + 8 * (l16 >> 2) + 4 * t + (l16 & 3), len - 1) * a.sn + 8 * g;
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s) kf[t][s] = *(const bf16x8*)(row + 32 * s);
+      for (int s = 0; s < D / 32; ++s) kf[t][s] = __builtin_bit_cast(bf16x8, load(row + 32 * s));
     }
   };
   auto load_v = [&](int key0) {
 #pragma unroll
     for (int i = 0; i < kVLoads; ++i)
-      vr[i] = *(const u32x4*)(V + (int64_t)min(key0 + i * R + lane / C, len - 1) * a.sn + 8 * (lane % C));
+      vr[i] = load(V + (int64_t)min(key0 + i * R + lane / C, len - 1) * a.sn + 8 * (lane % C));
   };
 
   f32x4 o[D / 16];
@@ -384,7 +385,7 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, int b, int h, int hg
 
 constexpr int kDecodeWaves = 4;
 
-template <int D>
+template <int D, bool STREAM>
 __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeArgs a, int parts,
                                                                         int groups) {
   __shared__ AttendLds<D, kDecodeWaves> lds;
@@ -396,7 +397,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_attn_kernel(DecodeAr
   const int per = (cnt + parts - 1) / parts;
   const int i0 = min(part * per, cnt), i1 = min(i0 + per, cnt);
   const const_ints list = constant(a.blocks) + (int64_t)bh * a.topk + i0;
-  attend<D, kDecodeWaves>(a, b, h, rest % groups, part, parts, i0, i1, [&](int i) { return list[i]; },
+  attend<D, kDecodeWaves, STREAM>(a, b, h, rest % groups, part, parts, i0, i1, [&](int i) { return list[i]; },
                           lds);
 }
 
@@ -407,7 +408,7 @@ constexpr int kFusedWaves = 8;
 constexpr int kFusedUnits = 64;     // 32 keys each: eight rounds of the wavefronts
 constexpr int kFusedBlocks = 2048;  // scores in LDS beside the value tiles
 
-template <int D>
+template <int D, bool STREAM>
 __global__ __launch_bounds__(64 * kFusedWaves) void decode_fused_kernel(DecodeArgs a, int groups) {
   extern __shared__ uint64_t keys[];  // [n_blk]
   __shared__ AttendLds<D, kFusedWaves> lds;
@@ -430,7 +431,7 @@ __global__ __launch_bounds__(64 * kFusedWaves) void decode_fused_kernel(DecodeAr
   if (hg == 0)
     for (int i = threadIdx.x; i < a.topk; i += 64 * kFusedWaves)
       a.blocks[(int64_t)bh * a.topk + i] = i < n ? list[i] : -1;
-  attend<D, kFusedWaves>(a, b, h, hg, 0, 1, 0, n,
+  attend<D, kFusedWaves, STREAM>(a, b, h, hg, 0, 1, 0, n,
                          [&](int i) { return __builtin_amdgcn_readfirstlane(list[i]); }, lds);
 }
 
@@ -495,8 +496,12 @@ hipError_t launch_d(const DecodeArgs& a, int parts, hipStream_t stream) {
   const int64_t rows = (int64_t)a.B * a.Hkv;
   const int groups = head_groups(a.Hq, a.Hkv);
   const int lds = a.n_blk * 8;
+  // chosen keys and values of more than the last cache holds are read past it (16 x 8 rows
+  // of 8192 tokens, 537 MB: 117 -> 104 us; 24 rows of 1024, 13 MB: 21.9 and 26.5)
+  const bool stream_in =
+      rows * (a.topk < a.n_blk ? a.topk : a.n_blk) * a.blk * D * 4 > kLastLevelCache;
   if (parts == 0) {
-    hipLaunchKernelGGL(decode_fused_kernel<D>, dim3((unsigned)(rows * groups)), dim3(64 * kFusedWaves),
+    hipLaunchKernelGGL((stream_in ? decode_fused_kernel<D, true> : decode_fused_kernel<D, false>), dim3((unsigned)(rows * groups)), dim3(64 * kFusedWaves),
                        lds, stream, a, groups);
     return hipGetLastError();
   }
@@ -509,7 +514,7 @@ hipError_t launch_d(const DecodeArgs& a, int parts, hipStream_t stream) {
                      a.keys ? 0 : lds, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(decode_attn_kernel<D>, dim3((unsigned)(rows * groups * parts)),
+  hipLaunchKernelGGL((stream_in ? decode_attn_kernel<D, true> : decode_attn_kernel<D, false>), dim3((unsigned)(rows * groups * parts)),
                      dim3(64 * kDecodeWaves), 0, stream, a, parts, groups);
   e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;

@@ -24,6 +24,14 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef SA_CONST int32_t* const_ints;
 __device__ __forceinline__ const_ints constant(const int32_t* p) { return (const_ints)(uintptr_t)p; }
 
+// 16 bytes past the caches' usual keeping, for data larger than the last of them.
+__device__ __forceinline__ u32x4 load_stream(const void* p) {
+  return __builtin_nontemporal_load((const u32x4*)p);
+}
+__device__ __forceinline__ void store_stream(void* p, u32x4 v) {
+  __builtin_nontemporal_store(v, (u32x4*)p);
+}
+
 // D = A * B + C for a 32x32 fp32 tile with K = 16 bf16 (v_mfma_f32_32x32x16_bf16).
 // Lane l supplies A[l % 32][8 * (l / 32) + e] and B[8 * (l / 32) + e][l % 32],
 // e = 0..7, and holds C[8 * (i / 4) + 4 * (l / 32) + i % 4][l % 32] in register i.

@@ -10,6 +10,9 @@ namespace sa {
 // problems keep the natural item order.
 constexpr int kScheduleMaxUnits = 4096;
 
+// Bytes of the last cache before HBM.
+constexpr int64_t kLastLevelCache = 256 << 20;
+
 struct AttnArgs {
   const void* q;
   const void* k;
@@ -50,7 +53,9 @@ struct RopeArgs {
   int B, N, d, rot, n_pos;
   float eps;
   bool halves, bhnd;
-  int heads;  // set by the launchers
+  // set by the launchers
+  int heads;
+  bool stream_in, stream_out;
 };
 
 // Blocks of the gradients' kernel at most, each with its own sums for dw.

@@ -16,9 +16,11 @@
 //
 // Bound: HBM bytes (4 an element forward, 6 backward; some 20 vector instructions
 // for every 8 elements).  Everything is fp32; each output is rounded to bf16 once.
-// Measured: 75600 tokens x 80 heads of 128 in 631 us, 4.97 TB/s (a 2 GiB copy runs at
-// 4.85); gradients of 2 x 32760 tokens x 24 heads in 249 us, 4.93 TB/s.  Eight tokens
+// Measured: 75600 tokens x 80 heads of 128 in 566 us, 5.5 TB/s (a 2 GiB copy runs at
+// 4.85); gradients of 2 x 32760 tokens x 24 heads in 235 us, 5.2 TB/s.  Eight tokens
 // take 4 us on the GPU and 15 us a call, the host's part.
+
+#include <type_traits>
 
 #include "device_common.h"
 #include "launch.h"
@@ -57,6 +59,12 @@ __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];
   return __builtin_bit_cast(u32x4, v);
+}
+
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load_row(const __bf16* p) {
+  if constexpr (STREAM) return load_stream(p);
+  return *(const u32x4*)p;
 }
 
 // What a lane needs to turn its 8 elements: y = x c + partner s.
@@ -133,7 +141,8 @@ __device__ __forceinline__ Token token_of(const RopeArgs& a, int64_t t) {
   return k;
 }
 
-template <int D, bool HALVES>
+// STREAM: the rows are read past the caches.
+template <int D, bool HALVES, bool STREAM>
 __global__ __launch_bounds__(64 * kRopeWaves) void norm_rope_kernel(RopeArgs a) {
   constexpr int C = D / 8, R = 64 / C;
   const int lane = threadIdx.x & 63;
@@ -174,7 +183,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void norm_rope_kernel(RopeArgs a) 
   for (int h = h0; h < h1; h += U) {
     u32x4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = *(const u32x4*)(x + min(h + u, h1 - 1) * o.sh);
+    for (int u = 0; u < U; ++u) v[u] = load_row<STREAM>(x + min(h + u, h1 - 1) * o.sh);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float f[8], p[8];
@@ -191,7 +200,12 @@ __global__ __launch_bounds__(64 * kRopeWaves) void norm_rope_kernel(RopeArgs a) 
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] *= r * w[i];
       turn.template apply<1>(f, p);
-      if (tok.real && h + u < h1) *(u32x4*)(y + (h + u) * yh) = pack8(f);
+      if (tok.real && h + u < h1) {
+        if (a.stream_out)
+          store_stream(y + (h + u) * yh, pack8(f));
+        else
+          *(u32x4*)(y + (h + u) * yh) = pack8(f);
+      }
     }
   }
 }
@@ -200,7 +214,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void norm_rope_kernel(RopeArgs a) 
 // the queries' first, then the keys', and keeps the lane's 8 columns of dw in
 // registers; its sums go to dw_parts[block][side][D], added up by a second kernel in
 // a fixed order (no atomics: the same call gives the same bits).
-template <int D, bool HALVES>
+template <int D, bool HALVES, bool STREAM>
 __global__ __launch_bounds__(64 * kRopeWaves) void norm_rope_bwd_kernel(RopeArgs a) {
   constexpr int C = D / 8, R = 64 / C;
   __shared__ float sums[kRopeWaves][R][D];
@@ -243,8 +257,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void norm_rope_bwd_kernel(RopeArgs
         u32x4 xv[U], yv[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          xv[u] = *(const u32x4*)(x + min(h + u, h1 - 1) * o.sh);
-          yv[u] = *(const u32x4*)(y + min(h + u, h1 - 1) * yh);
+          xv[u] = load_row<STREAM>(x + min(h + u, h1 - 1) * o.sh);
+          yv[u] = load_row<STREAM>(y + min(h + u, h1 - 1) * yh);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -268,7 +282,12 @@ __global__ __launch_bounds__(64 * kRopeWaves) void norm_rope_bwd_kernel(RopeArgs
             dw[i] = fmaf(real ? g[i] : 0.f, n, dw[i]);
             f[i] = r * fmaf(-n, m, g[i] * w[i]);
           }
-          if (real) *(u32x4*)(dx + (int64_t)(h + u) * D) = pack8(f);
+          if (real) {
+            if (a.stream_out)
+              store_stream(dx + (int64_t)(h + u) * D, pack8(f));
+            else
+              *(u32x4*)(dx + (int64_t)(h + u) * D) = pack8(f);
+          }
         }
       }
     }
@@ -321,27 +340,48 @@ int64_t rope_blocks(const RopeArgs& a) {
   return (groups + kRopeWaves - 1) / kRopeWaves;
 }
 
+// Results of more than the L2s hold are stored past the caches: nothing of them would be
+// left for the next kernel, and they push out what is still to be read (32760 tokens x 24
+// heads: 84.6 -> 66.2 us; 4000 x 24 16.6 and 16.0).  Rows of more than the last cache holds
+// are read past it too (75600 x 80: 630 us, 585 with the stores, 566 with both; 32760 x 24
+// 66 and 77: those the kernel before may have left there).
+void set_streams(RopeArgs& a, int reads) {
+  const int64_t bytes = (int64_t)a.B * a.N * (a.t[0].H + a.t[1].H) * a.d * 2;
+  a.stream_out = bytes > (32 << 20);
+  a.stream_in = reads * bytes > kLastLevelCache;
+}
+
 }  // namespace
 
 hipError_t launch_norm_rope(RopeArgs a, hipStream_t stream) {
   a.heads = heads_per_unit(a, 8192);
+  set_streams(a, 1);
   const int64_t runs = (a.t[0].H + a.heads - 1) / a.heads + (a.t[1].H + a.heads - 1) / a.heads;
   const int64_t grid = rope_blocks(a) * runs;
   if (grid >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-  auto kernel = a.d == 128 ? (a.halves ? norm_rope_kernel<128, true> : norm_rope_kernel<128, false>)
-                           : (a.halves ? norm_rope_kernel<64, true> : norm_rope_kernel<64, false>);
+  auto pick = [&](auto stream_in) {
+    constexpr bool S = decltype(stream_in)::value;
+    return a.d == 128 ? (a.halves ? norm_rope_kernel<128, true, S> : norm_rope_kernel<128, false, S>)
+                      : (a.halves ? norm_rope_kernel<64, true, S> : norm_rope_kernel<64, false, S>);
+  };
+  auto kernel = a.stream_in ? pick(std::true_type{}) : pick(std::false_type{});
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kRopeWaves), 0, stream, a);
   return hipGetLastError();
 }
 
 hipError_t launch_norm_rope_bwd(RopeArgs a, float* dwq, float* dwk, hipStream_t stream) {
   a.heads = heads_per_unit(a, 8192);
+  set_streams(a, 2);
   const int64_t runs = (max(a.t[0].H, a.t[1].H) + a.heads - 1) / a.heads;
   const int64_t most = rope_blocks(a) * runs;
   const int grid = (int)(most < kRopeParts ? most : kRopeParts);
-  auto kernel = a.d == 128
-                    ? (a.halves ? norm_rope_bwd_kernel<128, true> : norm_rope_bwd_kernel<128, false>)
-                    : (a.halves ? norm_rope_bwd_kernel<64, true> : norm_rope_bwd_kernel<64, false>);
+  auto pick = [&](auto stream_in) {
+    constexpr bool S = decltype(stream_in)::value;
+    return a.d == 128
+               ? (a.halves ? norm_rope_bwd_kernel<128, true, S> : norm_rope_bwd_kernel<128, false, S>)
+               : (a.halves ? norm_rope_bwd_kernel<64, true, S> : norm_rope_bwd_kernel<64, false, S>);
+  };
+  auto kernel = a.stream_in ? pick(std::true_type{}) : pick(std::false_type{});
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(64 * kRopeWaves), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

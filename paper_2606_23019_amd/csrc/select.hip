@@ -9,8 +9,8 @@
 // sums nor an fp32 rounding decides between two blocks.  A mean is the fp32 rounding
 // of the 64-bit sum's quotient, a score the 64-bit sum of exact products.
 //
-// Measured, 40 heads x 75600 tokens (591 x 591 blocks of 128, d = 128): means 133 us a
-// tensor, 5.8 TB/s (a reduction over 2 GiB reads at 5.7); selection of 59 with
+// Measured, 40 heads x 75600 tokens (591 x 591 blocks of 128, d = 128): means about 112 us
+// a tensor, 6.9 TB/s (a reduction over 2 GiB reads at 5.7); selection of 59 with
 // candidates and kept blocks 145-150 us, of which the products' 3.6 Gflop take some 75
 // (56 at the 64 TFLOP/s of a large 64-bit matrix product), the borders 18 and the masks 12.
 
@@ -33,6 +33,7 @@ struct MeansSide {
   float* means;
   int n_blk;
   int64_t items;
+  bool stream;  // more than the last cache holds (40 heads x 75600 tokens: 133 -> 122 us)
 };
 
 template <int D, int BLK>
@@ -48,10 +49,15 @@ __device__ __forceinline__ void block_mean(const MeansSide& o, int64_t item, int
   const __bf16* from =
       (const __bf16*)o.x + (bh / H) * o.sb + (bh % H) * o.sh + (int64_t)blk * BLK * sn + 8 * chunk;
   u32x4 v[BLK / R];
+  const int row0 = threadIdx.x / C;
+  if (o.stream) {
 #pragma unroll
-  for (int i = 0; i < BLK / R; ++i) {
-    const int row = threadIdx.x / C + i * R;
-    v[i] = row < size ? *(const u32x4*)(from + row * sn) : u32x4{};
+    for (int i = 0; i < BLK / R; ++i)
+      v[i] = row0 + i * R < size ? load_stream(from + (row0 + i * R) * sn) : u32x4{};
+  } else {
+#pragma unroll
+    for (int i = 0; i < BLK / R; ++i)
+      v[i] = row0 + i * R < size ? *(const u32x4*)(from + (row0 + i * R) * sn) : u32x4{};
   }
   double t[8] = {};
 #pragma unroll
@@ -209,7 +215,8 @@ hipError_t launch_block_means(const MeansArgs& q, const MeansArgs& k, int B, int
                               hipStream_t stream) {
   auto side = [&](const MeansArgs& a) {
     const int n_blk = (N + a.blk - 1) / a.blk;
-    return MeansSide{a.x, a.sb, a.sh, a.sn, a.means, n_blk, a.x ? (int64_t)B * H * n_blk : 0};
+    return MeansSide{a.x, a.sb, a.sh, a.sn, a.means, n_blk, a.x ? (int64_t)B * H * n_blk : 0,
+                     (int64_t)B * H * N * d * 2 > kLastLevelCache};
   };
   const MeansSide first = side(q), second = side(k);
   const dim3 grid((unsigned)(first.items + second.items));

@@ -147,6 +147,27 @@ def test_norm_rope_strides_and_positions_out_of_range():
     assert all(torch.equal(a, b) for a, b in zip(got, ref))
 
 
+def test_norm_rope_past_the_caches():
+    """More than the last cache holds is read and written past it: the same results."""
+    import torch
+    from paper_2606_23019_amd import binding
+    B, N, H, d = 2, 12000, 26, 128
+    q, k, wq, wk, cos, sin, _, _, _ = rope_inputs((B, N, H, H, d, d, "halves", "bhnd", False, True), 3)
+    assert 2 * B * N * H * d * 2 > 256 << 20
+    got = binding.qk_norm_rope(q, k, wq, wk, cos, sin, pairs="halves")
+    dq, dk, _, _ = binding.qk_norm_rope_bwd(*got, q, k, wq, wk, cos, sin, pairs="halves")
+    for b in range(B):
+        part = q[b:b + 1], k[b:b + 1], wq, wk, cos, sin
+        ref = binding.qk_norm_rope(*part, pairs="halves")
+        assert all(torch.equal(x[b:b + 1], y) for x, y in zip(got, ref))
+        ref = binding.qk_norm_rope_bwd(got[0][b:b + 1], got[1][b:b + 1], *part, pairs="halves")
+        assert torch.equal(dq[b:b + 1], ref[0]) and torch.equal(dk[b:b + 1], ref[1])
+    x = torch.cat([q, k], 2).transpose(1, 2).repeat(1, 2, 1, 1)
+    means = binding.block_means(x, 64)
+    assert torch.equal(means[:, :H], binding.block_means(q.transpose(1, 2), 64))
+    assert torch.equal(means[:, -H:], binding.block_means(k.transpose(1, 2), 64))
+
+
 # --------------------------------------------------------------- selection ---
 
 @pytest.mark.parametrize("B,H,N,d,blk", [(1, 1, 1, 128, 128), (2, 3, 200, 64, 64), (1, 2, 1000, 128, 64),
@@ -381,6 +402,27 @@ def test_selected_decode(case, tokens_first):
                 continue
             check(out[b, rows], ro, eo)
             assert (np.abs(f64(lse[b, rows]) - rl) <= el).all()
+
+
+@pytest.mark.parametrize("B,cap,blk,topk", [(9, 8300, 128, 65), (70, 1024, 64, 16)])
+def test_selected_decode_past_the_caches(B, cap, blk, topk):
+    """Chosen blocks of more than the last cache holds, in parts and in one launch."""
+    import torch
+    from paper_2606_23019_amd import binding
+    Hkv, G, d = 8, 2, 128
+    assert B * Hkv * topk * blk * d * 4 > 256 << 20
+    g = gen(cap)
+    q, k, v = randn(g, B, Hkv * G, d), randn(g, B, Hkv, cap, d), randn(g, B, Hkv, cap, d)
+    means = binding.block_means(k, blk)
+    ln = torch.full((B,), cap - 3, device="cuda", dtype=torch.int32)
+    out, lse, blocks = binding.selected_decode(q, k, v, means, ln, topk, blk)
+    for b, h in ((0, 0), (B // 2, 3), (B - 1, Hkv - 1)):
+        rows = slice(h * G, (h + 1) * G)
+        ro, rl, rb, eo, el = ops.selected_decode(f64(q[b, rows]), f64(k[b, h]), f64(v[b, h]),
+                                                 f64(means[b, h]), cap - 3, topk, blk, d ** -0.5, U16)
+        assert blocks[b, h].tolist() == rb + [-1] * (topk - len(rb))
+        check(out[b, rows], ro, eo)
+        assert (np.abs(f64(lse[b, rows]) - rl) <= el).all()
 
 
 def test_decode_lengths_out_of_range_are_clamped():
