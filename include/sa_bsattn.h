@@ -325,9 +325,10 @@ SA_API int sa_bsattn_plan_destroy(sa_plan_t plan);
  * its blocks, its gradients, and its form for single tokens.  None allocates,
  * synchronises or keeps anything: workspaces are the caller's, 256-byte aligned,
  * of the size that the _workspace function gives (0 for sizes that the call
- * refuses and where it needs none: NULL will do), need no initial values, and are free again when the call's work on
- * its stream is done.  Calls that overlap in time need workspaces of their own;
- * every call may be captured into a graph, whose replays need theirs.  The same
+ * refuses and where it needs none: NULL will do), need no initial values, and
+ * are free again when the call's work on its stream is done.  Calls that overlap
+ * in time need workspaces of their own; every call may be captured into a graph,
+ * whose replays need theirs.  The same
  * call gives the same bits: no sum goes by the order of arrival.
  * Strides count elements; they are whole multiples of 8, not negative (0 repeats
  * a row), and head-dim elements are contiguous.

@@ -745,7 +745,8 @@ def selected_attn_fwd(q, k, v, blk_q, blk_k, topk, candidates=None, keep=None, s
     mask = q.new_empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64)
     ws = _workspace(q, "sa_selected_attn_workspace", B, H, N, d, blk_q, blk_k)
     _run("sa_selected_attn_fwd", dev, stream,
-         (*ptrs, c_ptr, cb, k_ptr, kb, out.data_ptr(), lse.data_ptr(), mask.data_ptr(), _address(ws), B, H, N, d, blk_q, blk_k, int(topk), scale),
+         (*ptrs, c_ptr, cb, k_ptr, kb, out.data_ptr(), lse.data_ptr(), mask.data_ptr(), _address(ws),
+          B, H, N, d, blk_q, blk_k, int(topk), scale),
          (out, lse, mask, ws))
     return out, lse, mask
 

@@ -21,11 +21,12 @@
 // bwd_prep_kernel makes what both need of a row: lse in the exponent's unit and D,
 // negative, so that the accumulators of S and dP can start from them.
 //
-// Bound: matrix products.  Measured, 12 heads x 32760 tokens (d = 128, blocks of 128, density
-// about 0.13): 2.69-2.75 ms, 7 products at 1.10-1.13 PFLOP/s (the forward kernel 1.05-1.1;
-// a large library product 1.16-1.35, depending on the card); the 5 that the formulas need
-// would take 1.6-1.9 ms at the library's rate.  2 x 10 heads x 4000 tokens (d = 64, blocks of 64): 110 us, of which 95
-// in the two kernels at 0.79 PFLOP/s: there the exponentials take as long as the products.
+// Bound: matrix products.  Measured, 12 heads x 32760 tokens (d = 128, blocks of 128,
+// density about 0.13): 2.69-2.75 ms, 7 products at 1.10-1.13 PFLOP/s (the forward kernel
+// 1.05-1.1; a large library product 1.16-1.35, depending on the card); the 5 that the
+// formulas need would take 1.6-1.9 ms at the library's rate.  2 x 10 heads x 4000 tokens
+// (d = 64, blocks of 64): 110 us, of which 95 in the two kernels at 0.79 PFLOP/s: there the
+// exponentials take as long as the products.
 
 #include <math.h>
 
@@ -65,8 +66,7 @@ __device__ __forceinline__ bf16x8 columns_operand(const __bf16* tile, int r0, in
 // reads each just before its use (12 heads x 32760 tokens, d = 128: 2840 -> 2770 us; at d =
 // 64 the registers for it are not there, nor for the products by columns at 128).
 // A wavefront in these products gives way to one in its exponentials and the products
-// after them, which it waits for with more in flight (2740 -> 2670 us; the other way
-// round 2680).
+// after them, which it waits for with more in flight (2740 -> 2670 us; the reverse 2680).
 template <int D, bool AHEAD, typename B1>
 __device__ __forceinline__ void score_products(f32x16& s, f32x16& p, const __bf16* S, const __bf16* P,
                                                int r0, int lane, const bf16x8 (&b0)[D / 16], B1 b1) {
@@ -322,7 +322,9 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
       int item = 0;
       const bool in = mine(j, &item);
       const uint64_t on = __ballot(in);
-      if (in) seq[x + kXcds * (base + __popcll(on & ((1ull << lane) - 1ull)))] = make_int4(item, 0, count_of(item), -1);
+      if (in)
+        seq[x + kXcds * (base + __popcll(on & ((1ull << lane) - 1ull)))] =
+            make_int4(item, 0, count_of(item), -1);
       base += __popcll(on);
     }
   }

@@ -81,9 +81,9 @@ __device__ __forceinline__ void copy16_to_lds(uint32_t lds_byte_addr, const void
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %4 offset:0\n\t"
                  "global_load_lds_dwordx4 %1, %4 offset:1024\n\t"
                  "global_load_lds_dwordx4 %2, %4 offset:2048\n\t"
-                 "global_load_lds_dwordx4 %3, %4 offset:3072"
-                 ::"v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "{m0}"(m0)
-                 : "memory");
+                 "global_load_lds_dwordx4 %3, %4 offset:%6"
+                 ::"v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base), "{m0}"(m0),
+                 "n"(3 * 1024) : "memory");
   else if constexpr (COUNT == 2)
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %2 offset:%4\n\t"
                  "global_load_lds_dwordx4 %1, %2 offset:%5"
@@ -105,10 +105,10 @@ __device__ __forceinline__ void copy16_to_lds(uint32_t lds_byte_addr, const void
 // a plan holds 4 lane offsets, and each load adds its uniform row offset to
 // the scalar base address.  (Every real row is congruent mod 16 to the row
 // used for its swizzle: R (n - n mod 4) is a multiple of 16.)  The lane offsets
-// also hold 3072 - 1024 (i mod 4), which with the kCopyShift elements that the
+// also hold 1024 (3 - i mod 4), which with the kCopyShift elements that the
 // base addresses given to the copies lie below their tensors takes back the
 // 1024 (i mod 4) of the load instruction (copy16_to_lds).
-constexpr int kCopyShift = 3072 / 2;
+constexpr int kCopyShift = 3 * 1024 / 2;
 template <typename T, int D>
 struct CopyPlan {
   static constexpr int kRowsPerLoad = 64 / T::kChunksPerRow;

@@ -23,7 +23,7 @@
 
 #include <math.h>
 
-#include "device_common.h"
+#include "attn_tiles.h"
 #include "launch.h"
 #include "topk_border.h"
 
@@ -31,8 +31,6 @@ namespace sa {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.402823466e+38f;
 
 __device__ __forceinline__ int length_of(const DecodeArgs& a, int b) {
@@ -198,16 +196,6 @@ __device__ __forceinline__ float quad_sum(float x) {
   return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-// XOR of the 16-byte chunk index of a value tile's row: rows read together by a
-// transposing read (4 k .. 4 k + 3) differ in chunk pairs.
-template <int D>
-__device__ __forceinline__ int vswz(int r) {
-  if constexpr (D == 128)
-    return ((r & 3) << 2) | ((r >> 2) & 3);
-  else
-    return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
-}
-
 constexpr int kDecodeGroup = 16;  // query heads of a workgroup: one side of an MFMA tile
 
 // A wavefront takes units of 32 keys: S^T = K Q^T with keys straight from memory
@@ -321,7 +309,7 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, int b, int h, int hg
 #pragma unroll
     for (int i = 0; i < kVLoads; ++i) {
       const int r = i * R + lane / C;
-      lds_write_b128(vs + r * D + (((lane % C) ^ vswz<D>(r)) << 3), vr[i]);
+      lds_write_b128(vs + r * D + (((lane % C) ^ swz<D>(r)) << 3), vr[i]);
     }
     if (more) load_v(key1);
     // the wavefront's own writes and reads of LDS complete in order
@@ -329,8 +317,8 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, int b, int h, int hg
     for (int i = 0; i < D / 16; ++i) {
       const int dd = 16 * i + (lane & 3) * 4;
       const int r0 = 8 * g + (l16 >> 2), r1 = r0 + 4;
-      const bf16x4 lo = lds_read_tr16_b64(vs + r0 * D + (((dd >> 3) ^ vswz<D>(r0)) << 3) + (dd & 7));
-      const bf16x4 hi = lds_read_tr16_b64(vs + r1 * D + (((dd >> 3) ^ vswz<D>(r1)) << 3) + (dd & 7));
+      const bf16x4 lo = lds_read_tr16_b64(vs + r0 * D + (((dd >> 3) ^ swz<D>(r0)) << 3) + (dd & 7));
+      const bf16x4 hi = lds_read_tr16_b64(vs + r1 * D + (((dd >> 3) ^ swz<D>(r1)) << 3) + (dd & 7));
       const bf16x8 vf = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       o[i] = mfma16x16x32(vf, pf, o[i]);
     }
@@ -501,8 +489,8 @@ hipError_t launch_d(const DecodeArgs& a, int parts, hipStream_t stream) {
   const bool stream_in =
       rows * (a.topk < a.n_blk ? a.topk : a.n_blk) * a.blk * D * 4 > kLastLevelCache;
   if (parts == 0) {
-    hipLaunchKernelGGL((stream_in ? decode_fused_kernel<D, true> : decode_fused_kernel<D, false>), dim3((unsigned)(rows * groups)), dim3(64 * kFusedWaves),
-                       lds, stream, a, groups);
+    hipLaunchKernelGGL((stream_in ? decode_fused_kernel<D, true> : decode_fused_kernel<D, false>),
+                       dim3((unsigned)(rows * groups)), dim3(64 * kFusedWaves), lds, stream, a, groups);
     return hipGetLastError();
   }
   if (a.keys) {
@@ -514,8 +502,9 @@ hipError_t launch_d(const DecodeArgs& a, int parts, hipStream_t stream) {
                      a.keys ? 0 : lds, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((stream_in ? decode_attn_kernel<D, true> : decode_attn_kernel<D, false>), dim3((unsigned)(rows * groups * parts)),
-                     dim3(64 * kDecodeWaves), 0, stream, a, parts, groups);
+  hipLaunchKernelGGL((stream_in ? decode_attn_kernel<D, true> : decode_attn_kernel<D, false>),
+                     dim3((unsigned)(rows * groups * parts)), dim3(64 * kDecodeWaves), 0, stream, a, parts,
+                     groups);
   e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
   hipLaunchKernelGGL(decode_merge_kernel<D>, dim3((unsigned)(((int64_t)a.B * a.Hq + 3) / 4)),

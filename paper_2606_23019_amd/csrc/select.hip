@@ -117,7 +117,8 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
   // places here instead of the schedule's two launches.
   if (a.order) {
     const int64_t items = (int64_t)a.B * a.H * a.n_qb;
-    for (int64_t p = (int64_t)blockIdx.x * THREADS + threadIdx.x; p < items; p += (int64_t)gridDim.x * THREADS) {
+    const int64_t step = (int64_t)gridDim.x * THREADS;
+    for (int64_t p = (int64_t)blockIdx.x * THREADS + threadIdx.x; p < items; p += step) {
       int u;
       const int unit = xcd_slice(p, a.B * a.H, a.n_qb, &u);
       a.order[p] = unit * a.n_qb + u;
