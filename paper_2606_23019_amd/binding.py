@@ -491,7 +491,8 @@ _LAYOUTS = {"bhnd": SA_LAYOUT_BHND, "bnhd": SA_LAYOUT_BNHD}
 
 
 def _named(table, key, name):
-    _need(key in table, "%s must be one of %s, got %r" % (name, ", ".join(sorted(table)), key))
+    if key not in table:
+        raise ValueError("%s must be one of %s, got %r" % (name, ", ".join(sorted(table)), key))
     return table[key]
 
 
@@ -508,9 +509,8 @@ def _ptr(t, dtype, name, dev):
     """Address of a contiguous tensor on GPU ``dev``."""
     if not (isinstance(t, _torch().Tensor) and t.dtype == dtype and t.is_contiguous()):
         _dev_ptr(t, dtype, name)  # raises
-    if t.get_device() != dev:
-        _need(_device(t, name) == dev, "%s is on GPU %d, others are on GPU %d"
-              % (name, t.get_device(), dev))
+    if t.get_device() != dev and _device(t, name) != dev:
+        raise ValueError("%s is on GPU %d, others are on GPU %d" % (name, t.get_device(), dev))
     return t.data_ptr()
 
 
@@ -537,18 +537,18 @@ def _strides(*s):
 def _rows_ptr(t, name, dev):
     """Address and strides of bf16 rows whose last dimension is contiguous; the strides of the
     others (any order, 0 for a repeated row) in the tensor's order."""
-    torch = _torch()
     if _device(t, name) != dev:
         raise ValueError("%s is on GPU %d, others are on GPU %d" % (name, t.get_device(), dev))
-    if t.dtype != torch.bfloat16:
-        raise TypeError("%s must be %s, got %s" % (name, torch.bfloat16, t.dtype))
+    if t.dtype is not _torch().bfloat16:
+        raise TypeError("%s must be %s, got %s" % (name, _torch().bfloat16, t.dtype))
     (n0, n1, n2, n3), (s0, s1, s2, s3) = t.shape, t.stride()
-    _need(s3 == 1 or n3 == 1, "%s must be contiguous in its last dimension" % name)
+    if s3 != 1 and n3 != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
     # the stride of a dimension of one entry means nothing
     s0, s1, s2 = s0 if n0 > 1 else 0, s1 if n1 > 1 else 0, s2 if n2 > 1 else 0
     ptr = t.data_ptr()
-    _need((s0 | s1 | s2) % 8 == 0 and ptr % 16 == 0,
-          "%s: rows must be 16-byte aligned" % name)
+    if (s0 | s1 | s2) % 8 or ptr % 16:
+        raise ValueError("%s: rows must be 16-byte aligned" % name)
     return ptr, _strides(s0, s1, s2)
 
 
@@ -559,7 +559,7 @@ def _run(fn, dev, stream, args, made):
     if stream is None and torch.cuda.current_device() == dev:
         st = getattr(_LIB or load(), fn)(*args, _current_stream(dev))
     else:
-        _need(stream is None or stream.device_index == dev, "stream is not of GPU %d" % dev)
+        _need(stream is None or stream.device_index == dev, "stream is of another GPU")
         with torch.cuda.device(dev):
             now = torch.cuda.current_stream()
             if stream is not None and stream != now:
@@ -598,25 +598,27 @@ def _mask_arg(m, B, H, n_qb, n_kb, name):
     if m.dtype == torch.uint64:
         m = m.view(torch.int64)
     shape = (H, n_qb, (n_kb + 63) // 64)
-    batches = m.shape[0] if m.dim() == 4 else 1
-    _need(tuple(m.shape[-3:]) == shape and m.dim() in (3, 4) and batches in (1, B),
-          "%s has shape %s, expected %s, alone or for each batch entry" % (name, tuple(m.shape), shape))
-    return m, batches
+    if m.shape == shape:
+        return m, 1
+    if m.shape != (1,) + shape and m.shape != (B,) + shape:
+        raise ValueError("%s has shape %s, expected %s, alone or for each batch entry"
+                         % (name, tuple(m.shape), shape))
+    return m, m.shape[0]
 
 
 def _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs, layout):
     _need(q.dim() == 4 and k.dim() == 4, "q and k must be [B, N, heads, d]")
     B, N, Hq, d = q.shape
     B2, N2, Hk, d2 = k.shape
-    _need(B2 == B and N2 == N and d2 == d, "k has shape %s, expected [%d, %d, heads, %d]"
-          % (tuple(k.shape), B, N, d))
+    if not (B2 == B and N2 == N and d2 == d):
+        raise ValueError("k has shape %s, expected [%d, %d, heads, %d]" % (tuple(k.shape), B, N, d))
     _need(wq.shape == (d,) and wk.shape == (d,), "wq and wk must be [d]")
     _need(cos.dim() == 2 and cos.shape == sin.shape, "cos and sin must be [positions, rot / 2]")
     n_pos, half = cos.shape
-    if positions is None:
-        _need(n_pos >= N, "cos and sin have %d positions for %d tokens" % (n_pos, N))
-    else:
+    if positions is not None:
         _need(positions.shape == (B, N), "positions must be [B, N]")
+    elif n_pos < N:
+        raise ValueError("cos and sin have %d positions for %d tokens" % (n_pos, N))
     return (B, N, Hq, Hk, d, 2 * half, n_pos, _named(_PAIRS, pairs, "pairs"),
             _named(_LAYOUTS, layout, "layout"))
 
@@ -667,8 +669,9 @@ def qk_norm_rope_bwd(dq_out, dk_out, q, k, wq, wk, cos, sin, positions=None, eps
     B, N, Hq, Hk, d, rot, n_pos, pr, lay = _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs,
                                                         layout)
     for t, H, name in ((dq_out, Hq, "dq_out"), (dk_out, Hk, "dk_out")):
-        _need(t.shape == _heads_shape(lay, B, N, H, d), "%s has shape %s, expected %s"
-              % (name, tuple(t.shape), _heads_shape(lay, B, N, H, d)))
+        if t.shape != _heads_shape(lay, B, N, H, d):
+            raise ValueError("%s has shape %s, expected %s"
+                             % (name, tuple(t.shape), _heads_shape(lay, B, N, H, d)))
     dq, dk = q.new_empty((B, N, Hq, d)), q.new_empty((B, N, Hk, d))
     dwq, dwk = wq.new_empty(d), wq.new_empty(d)
     ws = _workspace(q, "sa_qk_norm_rope_bwd_workspace", d)
@@ -689,7 +692,7 @@ def block_means(x, blk, stream=None):
     _need(x.dim() == 4, "x must be [B, H, N, d]")
     ptr, strides = _rows_ptr(x, "x", dev)
     B, H, N, d = x.shape
-    _need(blk in (64, 128), "blk must be 64 or 128, got %r" % (blk,))
+    _need(blk in (64, 128), "blk must be 64 or 128")
     means = x.new_empty((B, H, -(-N // blk), d), dtype=_torch().float32)
     _run("sa_block_means", dev, stream, (ptr, strides, means.data_ptr(), B, H, N, d, blk), (means,))
     return means
@@ -708,8 +711,9 @@ def block_select(q_means, k_means, topk, candidates=None, keep=None, stream=None
     _need(q_means.dim() == 4 and k_means.dim() == 4, "q_means and k_means must be [B, H, blocks, d]")
     B, H, n_qb, d = q_means.shape
     B2, H2, n_kb, d2 = k_means.shape
-    _need(B2 == B and H2 == H and d2 == d, "k_means has shape %s, expected [%d, %d, blocks, %d]"
-          % (tuple(k_means.shape), B, H, d))
+    if not (B2 == B and H2 == H and d2 == d):
+        raise ValueError("k_means has shape %s, expected [%d, %d, blocks, %d]"
+                         % (tuple(k_means.shape), B, H, d))
     candidates, cb = _mask_arg(candidates, B, H, n_qb, n_kb, "candidates")
     keep, kb = _mask_arg(keep, B, H, n_qb, n_kb, "keep")
     c_ptr, k_ptr = _ptrs(dev, torch.int64, candidates=candidates, keep=keep)
@@ -732,7 +736,8 @@ def selected_attn_fwd(q, k, v, blk_q, blk_k, topk, candidates=None, keep=None, s
     ptrs = _ptrs(dev, torch.bfloat16, q=q, k=k, v=v)
     _need(q.dim() == 4, "q must be [B, H, N, d]")
     B, H, N, d = q.shape
-    _same_shape(q, (k, v), ("k", "v"))
+    if not (k.shape == v.shape == q.shape):
+        _same_shape(q, (k, v), ("k", "v"))
     _need(blk_q in (64, 128) and blk_k in (64, 128), "blk_q and blk_k must be 64 or 128")
     n_qb, n_kb = -(-N // blk_q), -(-N // blk_k)
     candidates, cb = _mask_arg(candidates, B, H, n_qb, n_kb, "candidates")
@@ -770,8 +775,9 @@ def bsattn_bwd(dout, q, k, v, out, lse, mask_bits, blk_q, blk_k, scale=None, lay
         B, H, N, d = q.shape
     else:
         B, N, H, d = q.shape
-    _same_shape(q, (dout, k, v, out), ("dout", "k", "v", "out"))
-    _need(lse.shape == (B, H, N), "lse must have shape %s" % ((B, H, N),))
+    if not (dout.shape == k.shape == v.shape == out.shape == q.shape):
+        _same_shape(q, (dout, k, v, out), ("dout", "k", "v", "out"))
+    _need(lse.shape == (B, H, N), "lse must be [B, H, N]")
     _need(blk_q in (64, 128) and blk_k in (64, 128), "blk_q and blk_k must be 64 or 128")
     if not isinstance(mask_bits, torch.Tensor):
         mask_bits = mask_to_device(mask_bits, q.device)
@@ -804,14 +810,15 @@ def selected_decode(q, k, v, means, lengths, topk, blk, scale=None, stream=None)
     B, Hq, d = q.shape
     B2, Hkv, cap, d2 = k.shape
     topk = int(topk)
-    _need(B2 == B and d2 == d and Hkv > 0 and Hq % Hkv == 0,
-          "k has shape %s, q %s" % (tuple(k.shape), tuple(q.shape)))
-    _need(v.shape == k.shape, "v has shape %s, expected %s" % (tuple(v.shape), tuple(k.shape)))
-    _need(strides[:] == v_strides[:], "k and v must have the same strides")
-    _need(blk in (64, 128), "blk must be 64 or 128, got %r" % (blk,))
+    if not (B2 == B and d2 == d and Hkv > 0 and Hq % Hkv == 0):
+        raise ValueError("k has shape %s, q %s" % (tuple(k.shape), tuple(q.shape)))
+    if v.shape != k.shape:
+        raise ValueError("v has shape %s, expected %s" % (tuple(v.shape), tuple(k.shape)))
+    _need(strides is v_strides or strides[:] == v_strides[:], "k and v must have the same strides")
+    _need(blk in (64, 128), "blk must be 64 or 128")
     _need(topk >= 1, "topk must be at least 1")
-    _need(means.shape == (B, Hkv, -(-cap // blk), d), "means must have shape %s"
-          % ((B, Hkv, -(-cap // blk), d),))
+    if means.shape != (B, Hkv, -(-cap // blk), d):
+        raise ValueError("means must have shape %s" % ((B, Hkv, -(-cap // blk), d),))
     _need(lengths.shape == (B,), "lengths must be [B]")
     if scale is None:
         scale = 1.0 / float(d) ** 0.5
