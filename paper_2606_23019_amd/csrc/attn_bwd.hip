@@ -18,15 +18,15 @@
 // tiles are read from LDS by rows for the first and transposed for the second.  P and
 // dS are rounded to bf16 there, which the products take.
 //
-// bwd_prep_kernel makes what both need of a row: lse in the exponent's unit and D,
-// negative, so that the accumulators of S and dP can start from them.
+// token_terms makes what both need of a row: lse in the exponent's unit and D, negative,
+// so that the accumulators of S and dP can start from them.
 //
 // Bound: matrix products.  Measured, 12 heads x 32760 tokens (d = 128, blocks of 128,
 // density about 0.13): 2.69-2.75 ms, 7 products at 1.10-1.13 PFLOP/s (the forward kernel
 // 1.05-1.1; a large library product 1.16-1.35, depending on the card); the 5 that the
 // formulas need would take 1.6-1.9 ms at the library's rate.  2 x 10 heads x 4000 tokens
-// (d = 64, blocks of 64): 110 us, of which 95 in the two kernels at 0.79 PFLOP/s: there the
-// exponentials take as long as the products.
+// (d = 64, blocks of 64): 108 us, of which 95-100 in the two kernels at 0.75-0.79 PFLOP/s:
+// there the exponentials take as long as the products.
 
 #include <math.h>
 
@@ -95,23 +95,16 @@ __device__ __forceinline__ void score_products(f32x16& s, f32x16& p, const __bf1
   }
 }
 
-// ---- preparation: lists of the mask's rows and columns, two floats a row ----
-// One launch of independent blocks: first those of the mask's rows (a wavefront each,
-// the key blocks of (h, u)), then of its columns (the query blocks whose row has bit
-// v), both ascending; then of rows[bh][n] = {-lse / scale, -D}, d / 8 lanes each
-// (past N {-inf, 0}, up to n_pad).
-struct PrepGrid {
-  int row_blocks, column_blocks, token_blocks;
-};
-
-template <int D>
-__global__ __launch_bounds__(256) void bwd_prep_kernel(BwdArgs a, PrepGrid grid) {
+// ---- lists of the mask's rows and columns ----
+// A wavefront each: first the rows (the key blocks of (h, u)), then the columns (the query
+// blocks whose row has bit v), both ascending.
+__global__ __launch_bounds__(256) void bwd_lists_kernel(BwdArgs a, int row_blocks) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint64_t below = (1ull << lane) - 1ull;
   const int W = (a.n_kb + 63) / 64;
-  int blk = blockIdx.x;
-  if (blk < grid.row_blocks) {
+  const int blk = blockIdx.x;
+  if (blk < row_blocks) {
     const int64_t row = (int64_t)blk * 4 + wave;
     if (row >= (int64_t)a.mask_heads * a.n_qb) return;
     const uint64_t* words = a.mask + row * W;
@@ -133,44 +126,21 @@ __global__ __launch_bounds__(256) void bwd_prep_kernel(BwdArgs a, PrepGrid grid)
     if (lane == 0) a.row_counts[row] = done;
     return;
   }
-  blk -= grid.row_blocks;
-  if (blk < grid.column_blocks) {
-    const int64_t col = (int64_t)blk * 4 + wave;
-    if (col >= (int64_t)a.mask_heads * a.n_kb) return;
-    const int64_t h = col / a.n_kb;
-    const int v = (int)(col - h * a.n_kb);
-    const uint64_t* word = a.mask + h * a.n_qb * W + v / 64;
-    int32_t* list = a.column_lists + col * a.n_qb;
-    int done = 0;
-    for (int u0 = 0; u0 < a.n_qb; u0 += 64) {
-      const int u = u0 + lane;
-      const bool on = u < a.n_qb && ((word[(int64_t)min(u, a.n_qb - 1) * W] >> (v & 63)) & 1ull);
-      const uint64_t all = __ballot(on);
-      if (on) list[done + __popcll(all & below)] = u;
-      done += __popcll(all);
-    }
-    if (lane == 0) a.column_counts[col] = done;
-    return;
+  const int64_t col = (int64_t)(blk - row_blocks) * 4 + wave;
+  if (col >= (int64_t)a.mask_heads * a.n_kb) return;
+  const int64_t h = col / a.n_kb;
+  const int v = (int)(col - h * a.n_kb);
+  const uint64_t* word = a.mask + h * a.n_qb * W + v / 64;
+  int32_t* list = a.column_lists + col * a.n_qb;
+  int done = 0;
+  for (int u0 = 0; u0 < a.n_qb; u0 += 64) {
+    const int u = u0 + lane;
+    const bool on = u < a.n_qb && ((word[(int64_t)min(u, a.n_qb - 1) * W] >> (v & 63)) & 1ull);
+    const uint64_t all = __ballot(on);
+    if (on) list[done + __popcll(all & below)] = u;
+    done += __popcll(all);
   }
-  blk -= grid.column_blocks;
-  constexpr int C = D / 8, R = 256 / C;
-  const int blocks = a.n_pad / R;
-  const int64_t bh = blk / blocks;
-  const int n = (blk - (int)bh * blocks) * R + threadIdx.x / C;
-  float t = 0.f;
-  if (n < a.N) {
-    const int64_t at = (bh / a.H) * a.sb + (bh % a.H) * a.sh + (int64_t)n * a.sn + 8 * (threadIdx.x % C);
-    const bf16x8 x = *(const bf16x8*)((const __bf16*)a.dout + at);
-    const bf16x8 y = *(const bf16x8*)((const __bf16*)a.out + at);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) t = fmaf((float)x[i], (float)y[i], t);
-  }
-#pragma unroll
-  for (int s = 1; s < C; s *= 2) t += __shfl_xor(t, s, 64);
-  if (threadIdx.x % C == 0) {
-    a.nlse[bh * a.n_pad + n] = n < a.N ? -a.lse[bh * a.N + n] / a.scale : -INFINITY;
-    a.ndelta[bh * a.n_pad + n] = -t;
-  }
+  if (lane == 0) a.column_counts[col] = done;
 }
 
 // ---- plan ----
@@ -203,14 +173,49 @@ struct PlanSide {
   int n_own, front, n_items, least;
 };
 
-__global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide columns, int mask_heads,
-                                                        int heads) {
+// What the two kernels need of a token: rows[bh][n] = {-lse / scale, -D}, past N {-inf, 0} up
+// to n_pad.  d / 8 lanes each.
+template <int D>
+__device__ __forceinline__ void token_terms(const BwdArgs& a, int blk) {
+  constexpr int C = D / 8, R = 1024 / C;
+  static_assert(128 % R == 0, "n_pad is a multiple of 128");
+  const int blocks = a.n_pad / R;
+  const int64_t bh = blk / blocks;
+  const int n = (blk - (int)bh * blocks) * R + threadIdx.x / C;
+  float t = 0.f;
+  if (n < a.N) {
+    const int64_t at = (bh / a.H) * a.sb + (bh % a.H) * a.sh + (int64_t)n * a.sn + 8 * (threadIdx.x % C);
+    const bf16x8 x = *(const bf16x8*)((const __bf16*)a.dout + at);
+    const bf16x8 y = *(const bf16x8*)((const __bf16*)a.out + at);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t = fmaf((float)x[i], (float)y[i], t);
+  }
+#pragma unroll
+  for (int s = 1; s < C; s *= 2) t += __shfl_xor(t, s, 64);
+  if (threadIdx.x % C == 0) {
+    a.nlse[bh * a.n_pad + n] = n < a.N ? -a.lse[bh * a.N + n] / a.scale : -INFINITY;
+    a.ndelta[bh * a.n_pad + n] = -t;
+  }
+}
+
+// The plan's workgroups, a sequence or the parts of a side each, and behind them those of the
+// tokens' terms, which take longer and hide it.
+constexpr int kPlanBlocks = 2 * (kXcds + 1);
+
+template <int D>
+__global__ __launch_bounds__(1024) void bwd_plan_kernel(BwdArgs a, PlanSide rows, PlanSide columns,
+                                                        int mask_heads, int heads) {
+  if (blockIdx.x >= kPlanBlocks) {
+    token_terms<D>(a, blockIdx.x - kPlanBlocks);
+    return;
+  }
+  const int place = blockIdx.x % (kXcds + 1);
   __shared__ int sums[1024];
   __shared__ int class_count[kClasses];
   __shared__ int staged[kStaged];  // the counts, where they fit
   __shared__ int seq_item[kSequence];
   __shared__ uint8_t seq_class[kSequence];
-  const PlanSide& o = blockIdx.y ? columns : rows;
+  const PlanSide& o = blockIdx.x > kXcds ? columns : rows;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int own = mask_heads * o.n_own;   // counts
   int t = 0;
@@ -233,7 +238,7 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
     const int bh = item / o.n_own;
     return counts[(int64_t)(bh % mask_heads) * o.n_own + (item - bh * o.n_own)];
   };
-  if (blockIdx.x == kXcds) {  // the parts, in the order of the items
+  if (place == kXcds) {  // the parts, in the order of the items
     if (o.front == 0) {
       if (tid == 0) *o.n_splits = 0;
       return;
@@ -280,7 +285,7 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(PlanSide rows, PlanSide 
     return;
   }
   // sequence x: a wavefront a class, which finds its members' number and then their places
-  const int x = blockIdx.x;
+  const int x = place;
   const int units = o.n_items / o.n_own;
   const int len = (o.n_items - x + kXcds - 1) / kXcds;
   int4* seq = o.table + o.front;
@@ -680,20 +685,19 @@ int64_t items_padded(int64_t items) { return (items + kXcds - 1) / kXcds * kXcds
 template <int D>
 hipError_t launch_d(const BwdArgs& a, const BwdWork& w, char* ws, hipStream_t stream) {
   const int64_t bh = (int64_t)a.B * a.H;
-  const PrepGrid grid{(int)(((int64_t)a.mask_heads * a.n_qb + 3) / 4),
-                      (int)(((int64_t)a.mask_heads * a.n_kb + 3) / 4),
-                      (int)(bh * (a.n_pad / (256 / (D / 8))))};
-  hipLaunchKernelGGL(bwd_prep_kernel<D>,
-                     dim3((unsigned)(grid.row_blocks + grid.column_blocks + grid.token_blocks)),
-                     dim3(256), 0, stream, a, grid);
+  const int row_blocks = (int)(((int64_t)a.mask_heads * a.n_qb + 3) / 4);
+  const int column_blocks = (int)(((int64_t)a.mask_heads * a.n_kb + 3) / 4);
+  hipLaunchKernelGGL(bwd_lists_kernel, dim3((unsigned)(row_blocks + column_blocks)), dim3(256), 0, stream,
+                     a, row_blocks);
   auto side = [&](const BwdSideWork& x, const int32_t* counts, int n_own) {
     return PlanSide{counts, (int4*)(ws + x.table), (int4*)(ws + x.splits), (int32_t*)(ws + x.n_splits),
                     n_own, x.front, (int)(bh * n_own), kLeast};
   };
   const PlanSide rows = side(w.rows, a.row_counts, a.n_qb);
   const PlanSide columns = side(w.columns, a.column_counts, a.n_kb);
-  hipLaunchKernelGGL(bwd_plan_kernel, dim3(kXcds + 1, 2), dim3(1024), 0, stream, rows, columns,
-                     a.mask_heads, (int)bh);
+  const int64_t token_blocks = bh * (a.n_pad / (1024 / (D / 8)));
+  hipLaunchKernelGGL(bwd_plan_kernel<D>, dim3((unsigned)(kPlanBlocks + token_blocks)), dim3(1024), 0, stream,
+                     a, rows, columns, a.mask_heads, (int)bh);
   const BwdSide r{a.row_lists, rows.table, rows.splits, rows.n_splits, (float*)(ws + w.rows.parts)};
   const BwdSide c{a.column_lists, columns.table, columns.splits, columns.n_splits,
                   (float*)(ws + w.columns.parts)};
