@@ -541,6 +541,8 @@ def _rows_ptr(t, name, dev):
         raise ValueError("%s is on GPU %d, others are on GPU %d" % (name, t.get_device(), dev))
     if t.dtype is not _torch().bfloat16:
         raise TypeError("%s must be %s, got %s" % (name, _torch().bfloat16, t.dtype))
+    if t.dim() != 4:
+        raise ValueError("%s must have four dimensions, got %d" % (name, t.dim()))
     (n0, n1, n2, n3), (s0, s1, s2, s3) = t.shape, t.stride()
     if s3 != 1 and n3 != 1:
         raise ValueError("%s must be contiguous in its last dimension" % name)
@@ -568,6 +570,13 @@ def _run(fn, dev, stream, args, made):
             _used_on(stream, *made)
     if st != SA_OK:
         raise SAError(fn, st)
+
+
+def _topk(topk):
+    topk = int(topk)
+    if not 1 <= topk < 1 << 31:
+        raise ValueError("topk must be at least 1 and a 32-bit number, got %d" % topk)
+    return topk
 
 
 def _current_stream(dev):
@@ -719,7 +728,8 @@ def block_select(q_means, k_means, topk, candidates=None, keep=None, stream=None
     c_ptr, k_ptr = _ptrs(dev, torch.int64, candidates=candidates, keep=keep)
     mask = q_means.new_empty((B, H, n_qb, (n_kb + 63) // 64), dtype=torch.int64)
     _run("sa_block_select", dev, stream,
-         (*ptrs, c_ptr, cb, k_ptr, kb, mask.data_ptr(), None, None, B, H, n_qb, n_kb, d, int(topk)), (mask,))
+         (*ptrs, c_ptr, cb, k_ptr, kb, mask.data_ptr(), None, None, B, H, n_qb, n_kb, d, _topk(topk)),
+         (mask,))
     return mask
 
 
@@ -751,7 +761,7 @@ def selected_attn_fwd(q, k, v, blk_q, blk_k, topk, candidates=None, keep=None, s
     ws = _workspace(q, "sa_selected_attn_workspace", B, H, N, d, blk_q, blk_k)
     _run("sa_selected_attn_fwd", dev, stream,
          (*ptrs, c_ptr, cb, k_ptr, kb, out.data_ptr(), lse.data_ptr(), mask.data_ptr(), _address(ws),
-          B, H, N, d, blk_q, blk_k, int(topk), scale),
+          B, H, N, d, blk_q, blk_k, _topk(topk), scale),
          (out, lse, mask, ws))
     return out, lse, mask
 
@@ -809,14 +819,13 @@ def selected_decode(q, k, v, means, lengths, topk, blk, scale=None, stream=None)
     v_ptr, v_strides = _rows_ptr(v, "v", dev)
     B, Hq, d = q.shape
     B2, Hkv, cap, d2 = k.shape
-    topk = int(topk)
+    topk = _topk(topk)
     if not (B2 == B and d2 == d and Hkv > 0 and Hq % Hkv == 0):
         raise ValueError("k has shape %s, q %s" % (tuple(k.shape), tuple(q.shape)))
     if v.shape != k.shape:
         raise ValueError("v has shape %s, expected %s" % (tuple(v.shape), tuple(k.shape)))
     _need(strides is v_strides or strides[:] == v_strides[:], "k and v must have the same strides")
     _need(blk in (64, 128), "blk must be 64 or 128")
-    _need(topk >= 1, "topk must be at least 1")
     if means.shape != (B, Hkv, -(-cap // blk), d):
         raise ValueError("means must have shape %s" % ((B, Hkv, -(-cap // blk), d),))
     _need(lengths.shape == (B,), "lengths must be [B]")

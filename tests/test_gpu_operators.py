@@ -491,6 +491,42 @@ def test_chain_eager_other_stream_and_captured(N, blk):
             assert all(torch.equal(a, b) for a, b in zip(outs, want)) and torch.isfinite(junk)
 
 
+def test_long_selections_and_decode_captured():
+    """Selections whose keys take more LDS than a kernel has by itself, and every form of the
+    single-token call, replayed in a graph on new inputs."""
+    import torch
+    from paper_2606_23019_amd import binding
+    g = gen(50)
+
+    def inputs():
+        return [torch.randn((1, 2, n, 128), generator=g, device="cuda") for n in (33, 900)] + [
+            randn(g, 2, 4, 64), randn(g, 2, 2, 140000, 64)]
+
+    def calls(qm, km, q, k):
+        outs = [binding.block_select(qm, km, 77)]
+        for cap, topk in ((3000, 9), (60000, 70), (140000, 70)):  # one launch, chosen apart, scored apart
+            kc = k[:, :, :cap]
+            ln = torch.full((2,), cap - 5, device="cuda", dtype=torch.int32)
+            outs += binding.selected_decode(q, kc, kc, binding.block_means(kc, 64), ln, topk, 64)
+        return outs
+    static = inputs()
+    calls(*static)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = calls(*static)
+    for _ in range(3):
+        new = inputs()
+        want = calls(*new)
+        for a, b in zip(static, new):
+            a.copy_(b)
+        torch.cuda.synchronize()
+        graph.replay()
+        junk = (new[0] * 2).sum()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)) and torch.isfinite(junk)
+
+
 def test_stream_argument():
     """A call on another stream waits for what made its inputs on the current one."""
     import torch

@@ -183,6 +183,11 @@ def test_binding_refuses_what_the_library_cannot_see():
     with pytest.raises(ValueError, match="is on GPU 1"):
         binding._rows_ptr(FakeGpu(x, 1), "x", 0)
     assert binding._ptr(FakeGpu(x), torch.bfloat16, "x", 0) == x.data_ptr()
+    with pytest.raises(ValueError, match="four dimensions"):
+        binding._rows_ptr(FakeGpu(x[0]), "x", 0)
+    for topk in (0, -1, 1 << 31, (1 << 32) + 1):
+        with pytest.raises(ValueError, match="topk must be"):
+            binding._topk(topk)
     with pytest.raises(ValueError, match="pairs must be"):
         binding._named(binding._PAIRS, "both", "pairs")
     for shape in ((1, 1, 1), (2, 2, 1), (2, 3, 1, 1), (2, 1, 1, 1, 1)):
