@@ -10,9 +10,12 @@
 // of the 64-bit sum's quotient, a score the 64-bit sum of exact products.
 //
 // Measured, 40 heads x 75600 tokens (591 x 591 blocks of 128, d = 128): means about 112 us
-// a tensor, 6.9 TB/s (a reduction over 2 GiB reads at 5.7); selection of 59 with
-// candidates and kept blocks 145-150 us, of which the products' 3.6 Gflop take some 75
-// (56 at the 64 TFLOP/s of a large 64-bit matrix product), the borders 18 and the masks 12.
+// a tensor, 6.9 TB/s (a reduction over 2 GiB reads at 5.7); selection of 59 with kept
+// blocks and candidates that leave half of the tiles 115-125 us (all of them 145-150: the
+// products' 3.6 Gflop take some 75, 56 at the 64 TFLOP/s of a large 64-bit matrix
+// product, the borders 18).
+
+#include <type_traits>
 
 #include "device_common.h"
 #include "launch.h"
@@ -100,8 +103,10 @@ constexpr int kSelectRows = 16;  // rows of a workgroup: one side of an MFMA til
 // v_mfma_f64_16x16x4, as ordered keys in LDS, then a wavefront a row picks.  Lane l
 // supplies row (or key block) l % 16 and, in step 4 s + e, the column 16 s + 4 (l / 16)
 // + e of both sides, so that its loads are 16 bytes; every key block's sum runs in the
-// same order, so equal blocks score alike.
-template <int D, int THREADS>
+// same order, so equal blocks score alike.  16 key blocks that are no row's candidates are
+// not scored at all (720p with frames that see the past: 368 -> 339 us); the candidate
+// words are requested a tile ahead.
+template <int D, int THREADS, bool CANDIDATES>
 __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int rows, int groups) {
   extern __shared__ uint64_t keys_all[];  // [rows][n_pad]
   const int lane = threadIdx.x & 63;
@@ -125,6 +130,18 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
     }
   }
 
+  const int h = bh % a.H;
+  const int words = (a.n_kb + 63) / 64;
+  // the candidate bits of rows 4 i + l / 16 from key block v0 on, whose words hold 16 more
+  uint64_t may[4] = {};
+  auto load_candidates = [&](int v0) {
+    const uint64_t* from = a.candidates + ((int64_t)(a.cand_per_batch ? bh : h) * a.n_qb + u0) * words;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      may[i] = v0 < a.n_kb ? from[min(4 * i + g, n_rows - 1) * words + v0 / 64] >> (v0 & 63) : 0;
+  };
+  if (CANDIDATES) load_candidates(wave * 16);
+
   const float* qrow = a.qm + ((int64_t)bh * a.n_qb + u0 + min(l16, n_rows - 1)) * D + 4 * g;
   const float* kmat = a.km + (int64_t)bh * a.n_kb * D + 4 * g;
   double qa[D / 4];
@@ -134,10 +151,18 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
 #pragma unroll
     for (int e = 0; e < 4; ++e) qa[4 * s + e] = v[e];
   }
-  const int h = bh % a.H;
-  const int words = (a.n_kb + 63) / 64;
   for (int v0 = wave * 16; v0 < a.n_kb; v0 += waves * 16) {
     const int v = v0 + l16;
+    uint64_t now[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) now[i] = may[i];
+    if constexpr (CANDIDATES) {
+      load_candidates(v0 + waves * 16);
+      if (!__any(((now[0] | now[1] | now[2] | now[3]) & 0xffff) != 0)) {
+        for (int row = g; row < n_rows; row += 4) keys_all[row * n_pad + v] = 0;
+        continue;
+      }
+    }
     const float* krow = kmat + (int64_t)min(v, a.n_kb - 1) * D;
     f32x4 kb[D / 16];
 #pragma unroll
@@ -152,7 +177,8 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = 4 * i + g;
-      if (row < n_rows) keys_all[row * n_pad + v] = order_key(c[i]);
+      if (row < n_rows)
+        keys_all[row * n_pad + v] = !CANDIDATES || ((now[i] >> l16) & 1ull) ? order_key(c[i]) : 0;
     }
   }
   __syncthreads();
@@ -160,8 +186,6 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
     const int64_t at = ((int64_t)bh * a.n_qb + u0 + row);
     const int64_t shared = ((int64_t)h * a.n_qb + u0 + row);
     // mask words, 64 at a time: lane l loads word w0 + l, and all take word i from lane i
-    const uint64_t* cand =
-        a.candidates ? a.candidates + (a.cand_per_batch ? at : shared) * words : nullptr;
     const uint64_t* keep = a.keep ? a.keep + (a.keep_per_batch ? at : shared) * words : nullptr;
     auto words_from = [&](const uint64_t* p, int w0) { return p && w0 + lane < words ? p[w0 + lane] : 0; };
     auto word_of = [](uint64_t mine, int i) {
@@ -170,12 +194,6 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
     };
     uint64_t* keys = keys_all + row * n_pad;
     uint64_t kept = words_from(keep, 0);
-    if (cand)
-      for (int w0 = 0; w0 < words; w0 += 64) {
-        const uint64_t mine = words_from(cand, w0);
-        for (int w = w0; w < min(w0 + 64, words); ++w)
-          if (64 * w + lane < a.n_kb && !((word_of(mine, w - w0) >> lane) & 1ull)) keys[64 * w + lane] = 0;
-      }
     Border edge;
     if (words <= 4)
       edge = border_of<4>(keys, a.n_kb, a.topk, lane);
@@ -247,8 +265,12 @@ hipError_t launch_block_select(const SelectArgs& a, hipStream_t stream) {
   // v_mfma_f64_4x4x4 spread a small problem further (one group 13.6 -> 9.5 us) but read
   // the key blocks four times as often (5 heads x 256 x 256 blocks: 15.0 -> 16.4 us).
   const bool few = grid <= 256;
-  auto kernel = a.d == 128 ? (few ? block_select_kernel<128, 1024> : block_select_kernel<128, 512>)
-                           : (few ? block_select_kernel<64, 1024> : block_select_kernel<64, 512>);
+  auto pick = [&](auto candidates) {
+    constexpr bool C = decltype(candidates)::value;
+    return a.d == 128 ? (few ? block_select_kernel<128, 1024, C> : block_select_kernel<128, 512, C>)
+                      : (few ? block_select_kernel<64, 1024, C> : block_select_kernel<64, 512, C>);
+  };
+  auto kernel = a.candidates ? pick(std::true_type{}) : pick(std::false_type{});
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute((const void*)kernel,
                                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
