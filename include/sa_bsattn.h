@@ -331,7 +331,9 @@ SA_API int sa_bsattn_plan_destroy(sa_plan_t plan);
  * whose replays need theirs.  The same
  * call gives the same bits: no sum goes by the order of arrival.
  * Strides count elements; they are whole multiples of 8, not negative (0 repeats
- * a row), and head-dim elements are contiguous.
+ * a row), and head-dim elements are contiguous.  Sizes that would take a launch of
+ * 2^32 threads or more are SA_ERR_UNSUPPORTED; the nearest line is the gradients',
+ * B H ceil(N / 128) of 2^21 at d = 128.
  */
 
 /* Which elements a rotation turns together. */

@@ -682,27 +682,41 @@ int front_of(int64_t items, int n_walked, int least) {
 
 int64_t items_padded(int64_t items) { return (items + kXcds - 1) / kXcds * kXcds; }
 
+// Workgroups of the launches.
+struct Grids {
+  int64_t row_lists, column_lists, plan, dq, dkv;
+};
+
+Grids grids_of(int64_t bh, int64_t mask_heads, int n_qb, int n_kb, int n_pad, int d, const BwdWork& w) {
+  return {(mask_heads * n_qb + 3) / 4, (mask_heads * n_kb + 3) / 4,
+          kPlanBlocks + bh * (n_pad / (1024 / (d / 8))), w.rows.front + items_padded(bh * n_qb),
+          w.columns.front + items_padded(bh * n_kb)};
+}
+
+// Every launch reads what the one before it wrote: none goes out behind one that failed.
 template <int D>
 hipError_t launch_d(const BwdArgs& a, const BwdWork& w, char* ws, hipStream_t stream) {
   const int64_t bh = (int64_t)a.B * a.H;
-  const int row_blocks = (int)(((int64_t)a.mask_heads * a.n_qb + 3) / 4);
-  const int column_blocks = (int)(((int64_t)a.mask_heads * a.n_kb + 3) / 4);
-  hipLaunchKernelGGL(bwd_lists_kernel, dim3((unsigned)(row_blocks + column_blocks)), dim3(256), 0, stream,
-                     a, row_blocks);
+  const Grids grids = grids_of(bh, a.mask_heads, a.n_qb, a.n_kb, a.n_pad, D, w);
+  const int row_blocks = (int)grids.row_lists;
+  hipLaunchKernelGGL(bwd_lists_kernel, dim3((unsigned)(grids.row_lists + grids.column_lists)), dim3(256), 0,
+                     stream, a, row_blocks);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   auto side = [&](const BwdSideWork& x, const int32_t* counts, int n_own) {
     return PlanSide{counts, (int4*)(ws + x.table), (int4*)(ws + x.splits), (int32_t*)(ws + x.n_splits),
                     n_own, x.front, (int)(bh * n_own), kLeast};
   };
   const PlanSide rows = side(w.rows, a.row_counts, a.n_qb);
   const PlanSide columns = side(w.columns, a.column_counts, a.n_kb);
-  const int64_t token_blocks = bh * (a.n_pad / (1024 / (D / 8)));
-  hipLaunchKernelGGL(bwd_plan_kernel<D>, dim3((unsigned)(kPlanBlocks + token_blocks)), dim3(1024), 0, stream,
-                     a, rows, columns, a.mask_heads, (int)bh);
+  hipLaunchKernelGGL(bwd_plan_kernel<D>, dim3((unsigned)grids.plan), dim3(1024), 0, stream, a, rows,
+                     columns, a.mask_heads, (int)bh);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
   const BwdSide r{a.row_lists, rows.table, rows.splits, rows.n_splits, (float*)(ws + w.rows.parts)};
   const BwdSide c{a.column_lists, columns.table, columns.splits, columns.n_splits,
                   (float*)(ws + w.columns.parts)};
-  const int dq_grid = (int)(rows.front + items_padded(rows.n_items));
-  const int dkv_grid = (int)(columns.front + items_padded(columns.n_items));
+  const int dq_grid = (int)grids.dq, dkv_grid = (int)grids.dkv;
   if (a.blk_q == a.blk_k) {
     const dim3 grid2((unsigned)(dq_grid + dkv_grid));
     if (a.blk_q == 128)
@@ -716,6 +730,8 @@ hipError_t launch_d(const BwdArgs& a, const BwdWork& w, char* ws, hipStream_t st
     hipLaunchKernelGGL((bwd_kernel<0, 128, D>), dim3(dkv_grid), dim3(256), 0, stream, a, r, c, dkv_grid);
     hipLaunchKernelGGL((bwd_kernel<64, 0, D>), dim3(dq_grid), dim3(128), 0, stream, a, r, c, 0);
   }
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
   auto join = [&](const BwdSide& x, const PlanSide& p, int blk, int results) {
     const int64_t waves = (int64_t)(p.front / 2) * (blk / 32) * (D / 32) * results;
     return JoinSide{x, p.n_own, blk, results, (int)((waves + 3) / 4)};
@@ -756,12 +772,16 @@ BwdWork bwd_work(int B, int H, int mask_heads, int n_qb, int n_kb, int n_pad, in
   w.rows.parts = take((size_t)w.rows.front * blk_q * d * 4);
   w.columns.parts = take((size_t)w.columns.front * blk_k * d * 8);
   w.total = at;
+  const Grids g = grids_of(bh, mask_heads, n_qb, n_kb, n_pad, d, w);
+  w.fits = launchable(g.row_lists + g.column_lists, 256) && launchable(g.plan, 1024) &&
+           launchable(g.dq + g.dkv, 256);
   return w;
 }
 
 hipError_t launch_attention_bwd(const BwdArgs& a, void* workspace, hipStream_t stream) {
   char* ws = (char*)workspace;
   const BwdWork w = bwd_work(a.B, a.H, a.mask_heads, a.n_qb, a.n_kb, a.n_pad, a.d, a.blk_q, a.blk_k);
+  if (!w.fits) return hipErrorInvalidValue;
   BwdArgs b = a;
   b.c_log2 = a.scale * kLog2e;
   b.row_counts = (int32_t*)(ws + w.rows.counts);

@@ -477,6 +477,8 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(DecodeArgs a, int par
   if (lane == 0) a.lse[row] = l != 0.f ? (m + fast_log2(l)) * kLn2 : -INFINITY;
 }
 
+int score_runs(int n_blk) { return (n_blk + kScoreRun - 1) / kScoreRun; }
+
 int head_groups(int Hq, int Hkv) { return (Hq / Hkv + kDecodeGroup - 1) / kDecodeGroup; }
 
 template <int D>
@@ -494,9 +496,11 @@ hipError_t launch_d(const DecodeArgs& a, int parts, hipStream_t stream) {
     return hipGetLastError();
   }
   if (a.keys) {
-    const int runs = (a.n_blk + kScoreRun - 1) / kScoreRun;
+    const int runs = score_runs(a.n_blk);
     hipLaunchKernelGGL(decode_score_kernel<D>, dim3((unsigned)(rows * runs)), dim3(kScoreThreads), 0,
                        stream, a, runs);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(decode_select_kernel<D>, dim3((unsigned)rows), dim3(kDecodeSelectThreads),
                      a.keys ? 0 : lds, stream, a);
@@ -522,6 +526,7 @@ constexpr int kScoredInPlace = 2048;
 DecodeWork decode_work(int B, int Hq, int Hkv, int n_blk, int topk, int blk, int d) {
   DecodeWork w{};
   const int64_t rows = (int64_t)B * Hkv * head_groups(Hq, Hkv);
+  w.fits = launchable(rows, 64 * kFusedWaves) && launchable((int64_t)B * Hkv, kDecodeSelectThreads);
   if ((int64_t)topk * (blk / 32) <= kFusedUnits && n_blk <= kFusedBlocks) return w;
   // a round of two workgroups a compute unit (16 x 8 rows of 64 blocks: 118.7 us in rounds
   // of half the length, 115.8)
@@ -531,6 +536,8 @@ DecodeWork decode_work(int B, int Hq, int Hkv, int n_blk, int topk, int blk, int
   if (w.parts > 1) w.total = ((size_t)B * Hq * w.parts * (d + 2) * 4 + 255) / 256 * 256;
   w.keys = w.total;
   w.scored = n_blk > kScoredInPlace;
+  w.fits = w.fits && launchable(rows * w.parts, 64 * kDecodeWaves) &&
+           (!w.scored || launchable((int64_t)B * Hkv * score_runs(n_blk), kScoreThreads));
   if (w.scored) w.total += (size_t)B * Hkv * n_blk * 8;
   return w;
 }
@@ -538,6 +545,7 @@ DecodeWork decode_work(int B, int Hq, int Hkv, int n_blk, int topk, int blk, int
 hipError_t launch_selected_decode(const DecodeArgs& args, void* workspace, hipStream_t stream) {
   DecodeArgs a = args;
   const DecodeWork w = decode_work(a.B, a.Hq, a.Hkv, a.n_blk, a.topk, a.blk, a.d);
+  if (!w.fits) return hipErrorInvalidValue;
   a.parts_out = (float*)workspace;
   a.keys = w.scored ? (uint64_t*)((char*)workspace + w.keys) : nullptr;
   return a.d == 128 ? launch_d<128>(a, w.parts, stream) : launch_d<64>(a, w.parts, stream);

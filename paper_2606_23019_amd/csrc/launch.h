@@ -10,6 +10,11 @@ namespace sa {
 // problems keep the natural item order.
 constexpr int kScheduleMaxUnits = 4096;
 
+// Whether HIP takes a launch of so many workgroups: fewer than 2^32 threads in all.
+constexpr bool launchable(int64_t workgroups, int threads) {
+  return workgroups <= (((int64_t)1 << 32) - 1) / threads;
+}
+
 // Bytes of the last cache before HBM.
 constexpr int64_t kLastLevelCache = 256 << 20;
 
@@ -61,6 +66,9 @@ struct RopeArgs {
 // Blocks of the gradients' kernel at most, each with its own sums for dw.
 constexpr int kRopeParts = 1024;
 
+// Whether the forward pass of this size can be launched (the gradients' always can).
+bool norm_rope_fits(RopeArgs a);
+
 hipError_t launch_norm_rope(RopeArgs a, hipStream_t stream);
 hipError_t launch_norm_rope_bwd(RopeArgs a, float* dwq, float* dwk, hipStream_t stream);
 
@@ -72,6 +80,9 @@ struct MeansArgs {
   float* means;
   int blk;
 };
+
+// `blocks`: of one tensor, or of both.
+bool block_means_fits(int64_t blocks);
 
 hipError_t launch_block_means(const MeansArgs& q, const MeansArgs& k, int B, int H, int N, int d,
                               hipStream_t stream);
@@ -91,6 +102,8 @@ struct SelectArgs {
   int B, H, n_qb, n_kb, d, topk;
   bool cand_per_batch, keep_per_batch;
 };
+
+bool block_select_fits(int64_t heads, int n_qb, int n_kb);
 
 hipError_t launch_block_select(const SelectArgs& a, hipStream_t stream);
 
@@ -117,6 +130,7 @@ struct DecodeArgs {
 struct DecodeWork {
   int parts;
   bool scored;
+  bool fits;  // the launches are of sizes that HIP takes
   size_t keys, total;
 };
 
@@ -169,6 +183,7 @@ struct BwdSideWork {
 struct BwdWork {
   BwdSideWork rows, columns;
   size_t nlse, ndelta, total;
+  bool fits;  // the launches are of sizes that HIP takes
 };
 
 BwdWork bwd_work(int B, int H, int mask_heads, int n_qb, int n_kb, int n_pad, int d, int blk_q,

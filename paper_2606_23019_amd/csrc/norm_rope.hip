@@ -340,6 +340,13 @@ int64_t rope_blocks(const RopeArgs& a) {
   return (groups + kRopeWaves - 1) / kRopeWaves;
 }
 
+// Workgroups of the forward pass, a.heads set.
+int64_t forward_grid(const RopeArgs& a) {
+  const int64_t runs =
+      ((int64_t)a.t[0].H + a.heads - 1) / a.heads + ((int64_t)a.t[1].H + a.heads - 1) / a.heads;
+  return rope_blocks(a) * runs;
+}
+
 // Results of more than the L2s hold are stored past the caches: nothing of them would be
 // left for the next kernel, and they push out what is still to be read (32760 tokens x 24
 // heads: 84.6 -> 66.2 us; 4000 x 24 16.6 and 16.0).  Rows of more than the last cache holds
@@ -353,12 +360,16 @@ void set_streams(RopeArgs& a, int reads) {
 
 }  // namespace
 
+bool norm_rope_fits(RopeArgs a) {
+  a.heads = heads_per_unit(a, 8192);
+  return launchable(forward_grid(a), 64 * kRopeWaves);
+}
+
 hipError_t launch_norm_rope(RopeArgs a, hipStream_t stream) {
   a.heads = heads_per_unit(a, 8192);
   set_streams(a, 1);
-  const int64_t runs = (a.t[0].H + a.heads - 1) / a.heads + (a.t[1].H + a.heads - 1) / a.heads;
-  const int64_t grid = rope_blocks(a) * runs;
-  if (grid >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+  const int64_t grid = forward_grid(a);
+  if (!launchable(grid, 64 * kRopeWaves)) return hipErrorInvalidValue;
   auto pick = [&](auto stream_in) {
     constexpr bool S = decltype(stream_in)::value;
     return a.d == 128 ? (a.halves ? norm_rope_kernel<128, true, S> : norm_rope_kernel<128, false, S>)

@@ -12,7 +12,7 @@
 
 namespace {
 
-constexpr int64_t kMaxGrid = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxInt = ((int64_t)1 << 31) - 1;
 
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
@@ -82,7 +82,7 @@ int rope_args(const void* q, const int64_t* q_strides, const void* k, const int6
       !aligned(cos, 16) || !aligned(sin, 16) || !aligned(positions, 4))
     return SA_ERR_INVALID_ARG;
   // a token's group and a run of heads are one workgroup's quarter at least
-  if ((int64_t)B * N >= ((int64_t)1 << 31) || cdiv((int64_t)B * N, 16) * ((int64_t)Hq + Hk) > kMaxGrid)
+  if ((int64_t)B * N >= ((int64_t)1 << 31) || cdiv((int64_t)B * N, 16) * ((int64_t)Hq + Hk) > kMaxInt)
     return SA_ERR_UNSUPPORTED;
   size_t q_bytes, k_bytes;
   if (!strided(q_strides, {B, N, Hq}, d, &q_bytes) || !strided(k_strides, {B, N, Hk}, d, &k_bytes))
@@ -121,7 +121,8 @@ int select_shape(int B, int H, int n_qb, int n_kb, int d, int topk) {
   if (B < 1 || H < 1 || n_qb < 1 || n_kb < 1 || topk < 1) return SA_ERR_INVALID_ARG;
   if (d != 64 && d != 128) return SA_ERR_UNSUPPORTED;
   if (n_kb > sa::kSelectMaxBlocks) return SA_ERR_UNSUPPORTED;
-  if ((int64_t)B * H * n_qb > kMaxGrid || (int64_t)B * H * n_kb > kMaxGrid) return SA_ERR_UNSUPPORTED;
+  if ((int64_t)B * H * n_qb > kMaxInt || (int64_t)B * H * n_kb > kMaxInt) return SA_ERR_UNSUPPORTED;
+  if (!sa::block_select_fits((int64_t)B * H, n_qb, n_kb)) return SA_ERR_UNSUPPORTED;
   return SA_OK;
 }
 
@@ -146,15 +147,16 @@ int attn_shape(int B, int H, int N, int d, int blk_q, int blk_k) {
   if (d != 64 && d != 128) return SA_ERR_UNSUPPORTED;
   if (!blk_ok(blk_q) || !blk_ok(blk_k)) return SA_ERR_UNSUPPORTED;
   if (cdiv(N, blk_k) > 65535 || cdiv(N, blk_q) > 65535) return SA_ERR_UNSUPPORTED;
-  if ((int64_t)B * H * cdiv(N, 8) > kMaxGrid) return SA_ERR_UNSUPPORTED;
+  if ((int64_t)B * H * cdiv(N, 8) > kMaxInt) return SA_ERR_UNSUPPORTED;
   return SA_OK;
 }
 
 int decode_shape(int B, int Hq, int Hkv, int cap, int d, int blk, int topk) {
   if (B < 1 || Hq < 1 || Hkv < 1 || cap < 1 || topk < 1 || Hq % Hkv) return SA_ERR_INVALID_ARG;
   if ((d != 64 && d != 128) || !blk_ok(blk)) return SA_ERR_UNSUPPORTED;
-  if (cdiv(cap, blk) > sa::kSelectMaxBlocks || (int64_t)cap + blk > kMaxGrid) return SA_ERR_UNSUPPORTED;
-  if ((int64_t)B * Hq * 1024 > kMaxGrid) return SA_ERR_UNSUPPORTED;
+  if (cdiv(cap, blk) > sa::kSelectMaxBlocks || (int64_t)cap + blk > kMaxInt) return SA_ERR_UNSUPPORTED;
+  if ((int64_t)B * Hq * 1024 > kMaxInt) return SA_ERR_UNSUPPORTED;
+  if (!sa::decode_work(B, Hq, Hkv, (int)cdiv(cap, blk), topk, blk, d).fits) return SA_ERR_UNSUPPORTED;
   return SA_OK;
 }
 
@@ -175,6 +177,7 @@ SA_API int sa_qk_norm_rope(const void* q, const int64_t* q_strides, const void* 
   if (!q_out || !k_out || !aligned(q_out, 16) || !aligned(k_out, 16)) return SA_ERR_INVALID_ARG;
   const Span outs[2] = {{q_out, (size_t)B * N * Hq * d * 2}, {k_out, (size_t)B * N * Hk * d * 2}};
   if (clash(outs, ins)) return SA_ERR_INVALID_ARG;
+  if (!sa::norm_rope_fits(a)) return SA_ERR_UNSUPPORTED;
   a.t[0].y = q_out;
   a.t[1].y = k_out;
   return status(sa::launch_norm_rope(a, (hipStream_t)stream));
@@ -220,7 +223,7 @@ SA_API int sa_block_means(const void* x, const int64_t* x_strides, float* means,
   if ((d != 64 && d != 128) || !blk_ok(blk)) return SA_ERR_UNSUPPORTED;
   if (!aligned(x, 16) || !aligned(means, 16)) return SA_ERR_INVALID_ARG;
   const int64_t blocks = (int64_t)B * H * cdiv(N, blk);
-  if ((int64_t)B * H > kMaxGrid || blocks > kMaxGrid || (int64_t)N + blk > kMaxGrid)
+  if ((int64_t)B * H > kMaxInt || !sa::block_means_fits(blocks) || (int64_t)N + blk > kMaxInt)
     return SA_ERR_UNSUPPORTED;
   size_t bytes;
   if (!strided(x_strides, {B, H, N}, d, &bytes)) return SA_ERR_INVALID_ARG;
@@ -253,8 +256,21 @@ SA_API int sa_block_select(const float* q_means, const float* k_means, const uin
   return status(sa::launch_block_select(a, (hipStream_t)stream));
 }
 
+// The means', the selection's and the attention's launches: the last has up to 2 blk_q
+// threads a query block, and some workgroups for the places that stay empty.
+static int selected_shape(int B, int H, int N, int d, int blk_q, int blk_k, int topk) {
+  int st = attn_shape(B, H, N, d, blk_q, blk_k);
+  if (st != SA_OK) return st;
+  const int64_t bh = (int64_t)B * H, n_qb = cdiv(N, blk_q), n_kb = cdiv(N, blk_k);
+  st = select_shape(B, H, (int)n_qb, (int)n_kb, d, topk);
+  if (st != SA_OK) return st;
+  if (!sa::block_means_fits(bh * (n_qb + n_kb)) || !sa::launchable(bh * n_qb + 64, 256))
+    return SA_ERR_UNSUPPORTED;
+  return SA_OK;
+}
+
 SA_API size_t sa_selected_attn_workspace(int B, int H, int N, int d, int blk_q, int blk_k) {
-  if (attn_shape(B, H, N, d, blk_q, blk_k) != SA_OK) return 0;
+  if (selected_shape(B, H, N, d, blk_q, blk_k, 1) != SA_OK) return 0;
   return selected_ws((int64_t)B * H, cdiv(N, blk_q), cdiv(N, blk_k), d).total;
 }
 
@@ -263,11 +279,9 @@ SA_API int sa_selected_attn_fwd(const void* q, const void* k, const void* v,
                                 const uint64_t* keep, int keep_batches, void* out, float* lse,
                                 uint64_t* mask_bits, void* workspace, int B, int H, int N, int d,
                                 int blk_q, int blk_k, int topk, float scale, void* stream) {
-  int st = attn_shape(B, H, N, d, blk_q, blk_k);
+  const int st = selected_shape(B, H, N, d, blk_q, blk_k, topk);
   if (st != SA_OK) return st;
   const int n_qb = (int)cdiv(N, blk_q), n_kb = (int)cdiv(N, blk_k);
-  st = select_shape(B, H, n_qb, n_kb, d, topk);
-  if (st != SA_OK) return st;
   if (!q || !k || !v || !out || !lse || !mask_bits || !workspace) return SA_ERR_INVALID_ARG;
   if (!scale_ok(scale)) return SA_ERR_INVALID_ARG;
   if (!batches_ok(candidates, candidate_batches, B) || !batches_ok(keep, keep_batches, B))
@@ -314,9 +328,10 @@ SA_API int sa_selected_attn_fwd(const void* q, const void* k, const void* v,
 SA_API size_t sa_bsattn_bwd_workspace(int B, int H, int N, int d, int blk_q, int blk_k,
                                       int mask_batches) {
   if (attn_shape(B, H, N, d, blk_q, blk_k) != SA_OK || (mask_batches != 1 && mask_batches != B)) return 0;
-  if ((int64_t)mask_batches * H * cdiv(N, blk_q) > kMaxGrid / cdiv(N, blk_k)) return 0;
-  return sa::bwd_work(B, H, mask_batches * H, (int)cdiv(N, blk_q), (int)cdiv(N, blk_k),
-                      (int)(cdiv(N, 128) * 128), d, blk_q, blk_k).total;
+  if ((int64_t)mask_batches * H * cdiv(N, blk_q) > kMaxInt / cdiv(N, blk_k)) return 0;
+  const sa::BwdWork w = sa::bwd_work(B, H, mask_batches * H, (int)cdiv(N, blk_q), (int)cdiv(N, blk_k),
+                                     (int)(cdiv(N, 128) * 128), d, blk_q, blk_k);
+  return w.fits ? w.total : 0;
 }
 
 SA_API int sa_bsattn_bwd(const void* dout, const void* q, const void* k, const void* v,
@@ -342,8 +357,10 @@ SA_API int sa_bsattn_bwd(const void* dout, const void* q, const void* k, const v
   const int n_qb = (int)cdiv(N, blk_q), n_kb = (int)cdiv(N, blk_k);
   const int n_pad = (int)(cdiv(N, 128) * 128);
   const int mask_heads = mask_batches * H;
-  if ((int64_t)mask_heads * n_qb > kMaxGrid / n_kb) return SA_ERR_UNSUPPORTED;
-  const size_t ws_bytes = sa::bwd_work(B, H, mask_heads, n_qb, n_kb, n_pad, d, blk_q, blk_k).total;
+  if ((int64_t)mask_heads * n_qb > kMaxInt / n_kb) return SA_ERR_UNSUPPORTED;
+  const sa::BwdWork work = sa::bwd_work(B, H, mask_heads, n_qb, n_kb, n_pad, d, blk_q, blk_k);
+  if (!work.fits) return SA_ERR_UNSUPPORTED;
+  const size_t ws_bytes = work.total;
   const size_t bytes = (size_t)B * H * N * d * 2;
   const Span ins[7] = {{dout, bytes}, {q, bytes}, {k, bytes}, {v, bytes}, {out, bytes},
                        {lse, (size_t)B * H * N * 4},

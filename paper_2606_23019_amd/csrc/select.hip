@@ -228,7 +228,15 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a, int
   }
 }
 
+// Rows of a workgroup whose keys LDS holds, 0 where it does not hold one.
+int rows_together(int n_kb) {
+  const int64_t rows = kSelectLds / (((int64_t)n_kb + 15) / 16 * 16 * 8);
+  return (int)(rows < kSelectRows ? rows : kSelectRows);
+}
+
 }  // namespace
+
+bool block_means_fits(int64_t blocks) { return launchable(blocks, 256); }
 
 hipError_t launch_block_means(const MeansArgs& q, const MeansArgs& k, int B, int H, int N, int d,
                               hipStream_t stream) {
@@ -238,6 +246,7 @@ hipError_t launch_block_means(const MeansArgs& q, const MeansArgs& k, int B, int
                      (int64_t)B * H * N * d * 2 > kLastLevelCache};
   };
   const MeansSide first = side(q), second = side(k);
+  if (!block_means_fits(first.items + second.items)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)(first.items + second.items));
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, first, second, H, N);
@@ -252,14 +261,17 @@ hipError_t launch_block_means(const MeansArgs& q, const MeansArgs& k, int B, int
   return hipGetLastError();
 }
 
+bool block_select_fits(int64_t heads, int n_qb, int n_kb) {
+  const int64_t rows = rows_together(n_kb);
+  return rows > 0 && launchable(heads * ((n_qb + rows - 1) / rows), 512);
+}
+
 hipError_t launch_block_select(const SelectArgs& a, hipStream_t stream) {
-  const int n_pad = (a.n_kb + 15) / 16 * 16;
-  int rows = kSelectLds / (n_pad * 8);
-  if (rows < 1) return hipErrorInvalidValue;
-  if (rows > kSelectRows) rows = kSelectRows;
+  if (!block_select_fits((int64_t)a.B * a.H, a.n_qb, a.n_kb)) return hipErrorInvalidValue;
+  const int rows = rows_together(a.n_kb);
   const int groups = (a.n_qb + rows - 1) / rows;
   const int64_t grid = (int64_t)a.B * a.H * groups;
-  const int lds = rows * n_pad * 8;
+  const int lds = rows * ((a.n_kb + 15) / 16 * 16) * 8;
   // up to a workgroup a compute unit, 16 wavefronts: a row each (24 heads x 63 x 63 blocks
   // 10.6 -> 9.2 us); more workgroups share the units.  Groups of four rows on
   // v_mfma_f64_4x4x4 spread a small problem further (one group 13.6 -> 9.5 us) but read
