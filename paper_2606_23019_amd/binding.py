@@ -544,6 +544,8 @@ def _rows_ptr(t, name, dev):
     if t.dim() != 4:
         raise ValueError("%s must have four dimensions, got %d" % (name, t.dim()))
     (n0, n1, n2, n3), (s0, s1, s2, s3) = t.shape, t.stride()
+    if max(n0, n1, n2) >= 1 << 31:  # the library's sizes are 32-bit numbers
+        raise ValueError("%s has a dimension of %d" % (name, max(n0, n1, n2)))
     if s3 != 1 and n3 != 1:
         raise ValueError("%s must be contiguous in its last dimension" % name)
     # the stride of a dimension of one entry means nothing
@@ -624,6 +626,8 @@ def _rope_shapes(q, k, wq, wk, cos, sin, positions, pairs, layout):
     _need(wq.shape == (d,) and wk.shape == (d,), "wq and wk must be [d]")
     _need(cos.dim() == 2 and cos.shape == sin.shape, "cos and sin must be [positions, rot / 2]")
     n_pos, half = cos.shape
+    if n_pos >= 1 << 31:
+        raise ValueError("cos and sin have %d positions" % n_pos)
     if positions is not None:
         _need(positions.shape == (B, N), "positions must be [B, N]")
     elif n_pos < N:

@@ -4,7 +4,7 @@ operators around the attention, before anything is enqueued; the sizes just belo
 import pytest
 
 from paper_2606_23019_amd import binding
-from test_operator_refusals import bwd, decode, means, select, selected, strides
+from test_operator_refusals import FakeGpu, bwd, decode, means, select, selected, strides
 
 UNSUPPORTED = binding.SA_ERR_UNSUPPORTED
 M = 1 << 20
@@ -59,3 +59,18 @@ def test_decode_of_more_scores_than_a_launch_takes(lib):
     assert lib.sa_selected_decode_workspace(M // 8, 1, 1, 16384 * 64, 64, 64, 99) == 0
     assert decode(lib, B=M // 8, Hq=1, Hkv=1, cap=16384 * 64, d=64, topk=99, s=strides(0, 0, 0)) == UNSUPPORTED
     assert lib.sa_selected_decode_workspace(M // 8 - 1, 1, 1, 16384 * 64, 64, 64, 99) > 0
+
+
+def test_binding_refuses_sizes_beyond_32_bits():
+    """The C ABI's sizes are ints: a larger one would arrive as another number."""
+    import torch
+    row = FakeGpu(torch.zeros((1, 1, 1, 64), dtype=torch.bfloat16))
+    n = (1 << 32) + 64
+    for shape in ((n, 1, 1, 64), (1, n, 1, 64), (1, 1, n, 64), (1, 1, 1 << 31, 64)):
+        with pytest.raises(ValueError, match="x has a dimension of"):
+            binding._rows_ptr(row.expand(shape), "x", 0)
+    assert list(binding._rows_ptr(row.expand(1, 1, (1 << 31) - 1, 64), "x", 0)[1]) == [0, 0, 0]
+    w = torch.zeros(64)
+    cos = torch.zeros((1, 32)).expand((1 << 32) + 1, 32)
+    with pytest.raises(ValueError, match="cos and sin have"):
+        binding._rope_shapes(row, row, w, w, cos, cos, torch.zeros((1, 1)).int(), "halves", "bhnd")
