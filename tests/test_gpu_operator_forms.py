@@ -1,0 +1,72 @@
+"""Forms of the operators around the attention that only larger problems take, against the float64
+reference: selections of more than 256 workgroups and their skip over tiles without candidates.
+Bounds as in tests/test_gpu_operators.py."""
+
+import numpy as np
+import pytest
+
+from oracle import operators as ops
+from test_gpu_operators import f64, gen, pack, unpack
+
+pytestmark = pytest.mark.gpu
+
+
+# --------------------------------------------------------------- selection ---
+
+def runs(kind, rng, shape):
+    """bool [..., n_qb, n_kb] whose rows have long runs without a bit."""
+    n_qb, n_kb = shape[-2:]
+    at = np.arange(n_kb)
+    end = (np.arange(n_qb) + 1) * n_kb // n_qb
+    if kind == "past":  # what lies before the row's end; nothing at all for the first rows
+        on = np.broadcast_to(at < end[:, None] - 5, shape).copy()
+    elif kind == "late":  # the first half is no row's
+        on = np.broadcast_to(at >= n_kb // 2 + 3, shape).copy()
+    else:  # "islands": a block here and there, tiles without any before, between and behind them
+        on = rng.random(shape) < 0.5
+        on &= (at // 16 % 5 == 2) | (at == n_kb - 1)
+        on[..., n_qb // 2, :] = False
+    return on
+
+
+FORMS = [  # B, H, n_qb, n_kb, d, topk, candidates, keep
+    (1, 40, 120, 100, 64, 9, None, None), (1, 40, 120, 100, 128, 17, None, "shared"),
+    (2, 20, 120, 250, 128, 30, ("past", "shared"), None), (2, 20, 120, 250, 64, 30, ("late", "own"), "own"),
+    (1, 40, 119, 591, 128, 59, ("past", "shared"), "shared"),
+    (1, 40, 119, 591, 64, 20, ("islands", "shared"), None),
+    (2, 20, 106, 1300, 128, 70, ("islands", "own"), "own"), (1, 40, 106, 1300, 64, 40, ("late", "shared"), None),
+    (1, 2, 150, 11000, 64, 100, ("past", "shared"), None), (2, 1, 150, 11000, 128, 100, None, "shared"),
+]
+
+
+FEW = [(1, 2, 33, 591, 128, 59, ("past", "shared"), None), (2, 2, 17, 300, 64, 12, ("islands", "own"), None),
+       (1, 3, 40, 1300, 128, 30, ("late", "own"), "shared"), (1, 1, 9, 6000, 64, 80, ("islands", "shared"), None)]
+
+
+@pytest.mark.parametrize("many,case", [(True, c) for c in FORMS] + [(False, c) for c in FEW])
+def test_block_select_forms(many, case):
+    import torch
+    from paper_2606_23019_amd import binding
+    B, H, n_qb, n_kb, d, topk, cand, keep = case
+    together = min(16, 156 * 1024 // (-(-n_kb // 16) * 16 * 8))
+    assert (B * H * -(-n_qb // together) > 256) == many  # the form's line
+    g = gen(n_kb + d)
+    qm, km = (torch.randn((B, H, n, d), generator=g, device="cuda") for n in (n_qb, n_kb))
+    km[:, :, n_kb // 2:] = km[:, :, :n_kb - n_kb // 2].clone()  # every score twice
+    rng = np.random.default_rng(n_kb)
+    con = kon = None
+    if cand:
+        con = runs(cand[0], rng, (B if cand[1] == "own" else 1, H, n_qb, n_kb))
+    if keep:
+        kon = rng.random((B if keep == "own" else 1, H, n_qb, n_kb)) < 0.02
+    bits = lambda on, kind: None if on is None else pack(on if kind == "own" else on[0])
+    mask = binding.block_select(qm, km, topk, candidates=bits(con, cand and cand[1]), keep=bits(kon, keep))
+    got = unpack(mask, n_kb)
+    for b in range(B):
+        for h in sorted({0, H // 3, H - 1}):
+            one = lambda on: None if on is None else on[b % len(on), h]
+            ref = ops.block_select(f64(qm[b, h]), f64(km[b, h]), topk, one(con), one(kon))
+            assert np.array_equal(got[b, h], ref), (b, h, np.argwhere(got[b, h] != ref)[:4])
+    # the other heads: as many blocks as there have to be
+    n = np.full((B, H, n_qb), min(topk, n_kb)) if con is None else np.minimum(con.sum(-1), topk)
+    assert (got.sum(-1) >= n).all() and (keep or (got.sum(-1) == n).all())
