@@ -1,12 +1,12 @@
 """Forms of the operators around the attention that only larger problems take, against the float64
-reference: selections of more than 256 workgroups and their skip over tiles without candidates.
-Bounds as in tests/test_gpu_operators.py."""
+reference: selections of more than 256 workgroups and their skip over tiles without candidates, and
+gradients whose lists are walked whole.  Bounds as in tests/test_gpu_operators.py."""
 
 import numpy as np
 import pytest
 
 from oracle import operators as ops
-from test_gpu_operators import f64, gen, pack, unpack
+from test_gpu_operators import U16, check, f64, gen, pack, randn, unpack
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +70,57 @@ def test_block_select_forms(many, case):
     # the other heads: as many blocks as there have to be
     n = np.full((B, H, n_qb), min(topk, n_kb)) if con is None else np.minimum(con.sum(-1), topk)
     assert (got.sum(-1) >= n).all() and (keep or (got.sum(-1) == n).all())
+
+
+# --------------------------------------------------------------- gradients ---
+
+WHOLE = [  # B, H, N, d, blk_q, blk_k, layout, a mask for every batch entry
+    (1, 40, 1500, 64, 64, 64, "bhnd", False), (1, 40, 1530, 128, 64, 64, "bnhd", False),
+    (2, 20, 3000, 128, 128, 128, "bhnd", True), (1, 40, 3001, 64, 128, 128, "bnhd", False),
+    (2, 24, 2990, 128, 128, 64, "bhnd", False), (1, 48, 2990, 64, 128, 64, "bhnd", False),
+    (2, 24, 3050, 128, 64, 128, "bnhd", True), (1, 48, 3050, 64, 64, 128, "bhnd", False),
+]
+
+
+@pytest.mark.parametrize("case", WHOLE)
+def test_bsattn_bwd_of_whole_lists(case):
+    """More than 1024 pairs of blocks in all: lists up to a 512th of them are walked by one
+    workgroup, longer ones (a row that sees all, a column that all see) are cut and joined."""
+    import torch
+    from paper_2606_23019_amd import binding
+    B, H, N, d, blk_q, blk_k, layout, own = case
+    g = gen(N + d)
+    shape = (B, H, N, d) if layout == "bhnd" else (B, N, H, d)
+    q, k, v, dout = (randn(g, *shape) for _ in range(4))
+    n_qb, n_kb = -(-N // blk_q), -(-N // blk_k)
+    rng = np.random.default_rng(N + d)
+    # few blocks in most heads, so that the lists of others are long beside a 512th of all
+    rho = np.where(np.arange(H) % 8 == 3, 0.55, rng.uniform(0.05, 0.4, H))
+    on = rng.random((B if own else 1, H, n_qb, n_kb)) < rho[None, :, None, None]
+    on[:, 0::5, n_qb - 2] = True
+    on[:, 0::5, :, n_kb // 3] = True
+    on[:, 1::5, 2] = False
+    on[:, :, n_qb - 1, n_kb - 1] = True  # the ragged corner
+    total = on.sum() * (1 if own else B)
+    limit = max(2, -(-total // 512))
+    sides = [on.sum(axis) for axis in (-1, -2)]
+    for lists in sides:
+        assert ((lists > 2) & (lists <= limit)).sum() > lists.size // 2 and lists[lists <= limit].max() >= 8
+    cut = [(lists > limit).any() for lists in sides]
+    assert all(cut) if blk_q == blk_k else any(cut)
+    heads = (lambda t: t) if layout == "bhnd" else (lambda t: t.transpose(1, 2))
+    out, lse = torch.empty_like(q), torch.empty((B, H, N), device="cuda")
+    for b in range(B):  # the forward call has one mask for all of its batch entries
+        fwd = binding.bsattn_fwd if layout == "bhnd" else binding.bsattn_fwd_bnhd
+        o, l = fwd(*(t[b:b + 1].contiguous() for t in (q, k, v)), pack(on[b if own else 0]), blk_q, blk_k)
+        out[b], lse[b] = o[0], l[0]
+    mask = pack(on if own else on[0])
+    got = binding.bsattn_bwd(dout, q, k, v, out, lse, mask, blk_q, blk_k, layout=layout)
+    again = binding.bsattn_bwd(dout, q, k, v, out, lse, mask, blk_q, blk_k, layout=layout)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+    for b, h in ((0, 0), (B - 1, 3), (B - 1, H - 4)):
+        see = on[b if own else 0, h].repeat(blk_q, 0)[:N].repeat(blk_k, 1)[:, :N]
+        x = [f64(heads(t)[b, h]) for t in (dout, q, k, v, out)]
+        ref, bound = ops.attention_grad(*x, f64(lse[b, h]), see, d ** -0.5, U16)
+        for t, r, e in zip(got, ref, bound):
+            check(heads(t)[b, h], r, e)
