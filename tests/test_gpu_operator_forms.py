@@ -1,6 +1,6 @@
 """Forms of the operators around the attention that only larger problems take, against the float64
-reference: selections of more than 256 workgroups and their skip over tiles without candidates, and
-gradients whose lists are walked whole.  Bounds as in tests/test_gpu_operators.py."""
+reference: selections of more than 256 workgroups and their skip over tiles without candidates, gradients
+whose lists are walked whole, and single tokens over long tables in one launch.  Bounds as in tests/test_gpu_operators.py."""
 
 import numpy as np
 import pytest
@@ -124,3 +124,38 @@ def test_bsattn_bwd_of_whole_lists(case):
         ref, bound = ops.attention_grad(*x, f64(lse[b, h]), see, d ** -0.5, U16)
         for t, r, e in zip(got, ref, bound):
             check(heads(t)[b, h], r, e)
+
+
+# ------------------------------------------------------------ single tokens ---
+
+LONG = [  # B, Hq, Hkv, cap, d, blk, topk, lengths: up to 64 units of 32 keys, 2048 blocks
+    (2, 2, 1, 131072, 128, 64, 32, [131072, 100001]), (1, 2, 2, 262140, 128, 128, 16, [262100]),
+    (2, 17, 1, 90001, 128, 64, 20, [90001, 81930]), (1, 1, 1, 131072, 64, 64, 32, [131071]),
+    (2, 4, 4, 40000, 128, 64, 9, [40000, 20000]), (3, 8, 2, 20000, 128, 64, 32, [20000, 16400, 2100]),
+    (1, 3, 1, 70000, 128, 128, 16, [69999]),
+]
+
+
+@pytest.mark.parametrize("case", LONG)
+def test_decode_in_one_launch_over_long_tables(case):
+    import torch
+    from paper_2606_23019_amd import binding
+    B, Hq, Hkv, cap, d, blk, topk, lengths = case
+    assert topk * blk // 32 <= 64 and -(-cap // blk) <= 2048  # the form's lines
+    g = gen(cap)
+    q, k, v = randn(g, B, Hq, d), randn(g, B, Hkv, cap, d), randn(g, B, Hkv, cap, d)
+    means = binding.block_means(k, blk)
+    for b, n in enumerate(lengths):  # nothing past the last token is read
+        k[b, :, n:], v[b, :, n:] = float("nan"), float("nan")
+        means[b, :, -(-n // blk) - 1:] = float("nan")
+    ln = torch.tensor(lengths, device="cuda", dtype=torch.int32)
+    out, lse, blocks = binding.selected_decode(q, k, v, means, ln, topk, blk)
+    G = Hq // Hkv
+    for b, n in enumerate(lengths):
+        for h in range(Hkv):
+            rows = slice(h * G, (h + 1) * G)
+            ro, rl, rb, eo, el = ops.selected_decode(f64(q[b, rows]), f64(k[b, h]), f64(v[b, h]),
+                                                     f64(means[b, h]), n, topk, blk, d ** -0.5, U16)
+            assert blocks[b, h].tolist() == rb + [-1] * (topk - len(rb))
+            check(out[b, rows], ro, eo)
+            assert (np.abs(f64(lse[b, rows]) - rl) <= el).all()
