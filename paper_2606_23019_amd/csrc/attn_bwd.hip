@@ -30,6 +30,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 #include "attn_tiles.h"
 #include "launch.h"
 #include "topk_border.h"
@@ -656,16 +658,29 @@ union BwdLds {
 };
 
 template <int BQ, int BK, int D>
-__global__ __launch_bounds__((BQ ? BQ : BK) * 2, D == 64 ? 3 : 2) void bwd_kernel(BwdArgs a, BwdSide rows,
-                                                                   BwdSide columns, int dkv_places) {
+using LdsOf = std::conditional_t<BQ == 0, DkvLds<BK ? BK : BQ, D>,
+                                 std::conditional_t<BK == 0, DqLds<BQ ? BQ : BK, D>, BwdLds<BQ, BK, D>>>;
+
+// Wavefronts on a SIMD that the registers have to leave room for: as many as LDS allows
+// workgroups of, up to three at d = 64 and two at 128.  Blocks of 64 at d = 64 have two (34 KB
+// of tiles for two wavefronts: four workgroups on a compute unit), dQ alone with blocks of 64
+// two or three.
+template <int BQ, int BK, int D>
+constexpr int kResident = [] {
+  constexpr int waves = (BQ ? BQ : BK) / 32, most = D == 64 ? 3 : 2;
+  const int by_lds = (160 * 1024 / (int)sizeof(LdsOf<BQ, BK, D>) * waves + 3) / 4;
+  return by_lds < most ? by_lds : most;
+}();
+
+template <int BQ, int BK, int D>
+__global__ __launch_bounds__((BQ ? BQ : BK) * 2, (kResident<BQ, BK, D>)) void bwd_kernel(
+    BwdArgs a, BwdSide rows, BwdSide columns, int dkv_places) {
+  __shared__ LdsOf<BQ, BK, D> lds;
   if constexpr (BQ == 0) {
-    __shared__ DkvLds<BK, D> lds;
     bwd_dkv<BK, D>(a, columns, blockIdx.x, lds);
   } else if constexpr (BK == 0) {
-    __shared__ DqLds<BQ, D> lds;
     bwd_dq<BQ, D>(a, rows, blockIdx.x, lds);
   } else {
-    __shared__ BwdLds<BQ, BK, D> lds;
     if ((int)blockIdx.x < dkv_places)
       bwd_dkv<BK, D>(a, columns, blockIdx.x, lds.dkv);
     else
