@@ -347,14 +347,16 @@ int64_t forward_grid(const RopeArgs& a) {
   return rope_blocks(a) * runs;
 }
 
-// Results of more than the L2s hold are stored past the caches: nothing of them would be
-// left for the next kernel, and they push out what is still to be read (32760 tokens x 24
-// heads: 84.6 -> 66.2 us; 4000 x 24 16.6 and 16.0).  Rows of more than the last cache holds
-// are read past it too (75600 x 80: 630 us, 585 with the stores, 566 with both; 32760 x 24
-// 66 and 77: those the kernel before may have left there).
+// Results of more than the last cache holds are stored past the caches, rows of more than it
+// holds read past it: nothing of them would be left for the next kernel, and they push out
+// what is still to be read (75600 tokens x 80 heads: 630 us, 585 with the stores, 566 with
+// both).  Below that the next kernel finds them there: with results of 201 MB (32760 x 24)
+// stored past the caches the call alone, over and over into the same memory, takes 65 us
+// instead of 81, but with the means of its q and k behind it 114 and 110, with the selected
+// attention 540 and 533; gradients and a sum of them 188 and 161.
 void set_streams(RopeArgs& a, int reads) {
   const int64_t bytes = (int64_t)a.B * a.N * (a.t[0].H + a.t[1].H) * a.d * 2;
-  a.stream_out = bytes > (32 << 20);
+  a.stream_out = bytes > kLastLevelCache;
   a.stream_in = reads * bytes > kLastLevelCache;
 }
 
