@@ -408,7 +408,8 @@ SA_API int sa_block_select(const float* q_means, const float* k_means, const uin
  * Attention over blocks that the means select: sa_block_means of q and k,
  * sa_block_select of them, and the attention over the selection, whose mask
  * [B][H][n_qb][W] is an output too.  out and lse are bit for bit those of
- * sa_bsattn_fwd with B H heads, one batch entry and that mask.
+ * sa_bsattn_fwd with B H heads, one batch entry and that mask, whose probabilities
+ * are rounded to bf16 for the product with v; their sum and lse are fp32.
  */
 SA_API size_t sa_selected_attn_workspace(int B, int H, int N, int d, int blk_q, int blk_k);
 
@@ -453,7 +454,9 @@ SA_API int sa_bsattn_bwd(const void* dout, const void* q, const void* k, const v
  * token}, both alike; means: float32 [B][Hkv][ceil(cap / blk)][d], of the
  * complete blocks (sa_block_means; others are not read); lengths: int32 [B];
  * lse: float32 [B][Hq]; blocks: int32 [B][Hkv][topk], the blocks taken, ascending,
- * then -1.  Tokens past lengths[b] are not read.  d, blk in {64, 128};
+ * then -1.  Tokens past lengths[b] are not read.  Probabilities are rounded to
+ * bf16 for the product with v (out is off by up to 2^-8 sum_j P_j |v_j| for it,
+ * beside its own rounding); their sum and lse are fp32.  d, blk in {64, 128};
  * ceil(cap / blk) <= 16384.
  */
 SA_API size_t sa_selected_decode_workspace(int B, int Hq, int Hkv, int cap, int d, int blk, int topk);

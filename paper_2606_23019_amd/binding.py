@@ -483,8 +483,10 @@ class Plan:
 #
 # Tensors may be on any GPU, all on the same one; the work goes to that GPU's
 # current stream, or to ``stream``, which has to be of that GPU and then waits
-# for the current one.  The checks are written for small calls, which take the
-# host longer than the GPU.
+# for the current one (the functions above leave that wait to the caller).  Inputs
+# that the caller frees before ``stream`` is done with them need
+# ``Tensor.record_stream`` there, as with the functions above.  The checks are
+# written for small calls, which take the host longer than the GPU.
 
 _PAIRS = {"interleaved": SA_PAIRS_INTERLEAVED, "halves": SA_PAIRS_HALVES}
 _LAYOUTS = {"bhnd": SA_LAYOUT_BHND, "bnhd": SA_LAYOUT_BNHD}

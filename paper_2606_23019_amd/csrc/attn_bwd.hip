@@ -160,7 +160,9 @@ __global__ __launch_bounds__(256) void bwd_lists_kernel(BwdArgs a, int row_block
 // blocks of 64) and 12 x 16000 (64 x 128), us: two classes 127 and 875, four 117 and 822,
 // sixteen 120 and 795 (12 x 32760: 2872, 2845, 2816-2880); limits of half the size 12 x
 // 8000 224 -> 276.
-constexpr int kPlaces = 512;            // two workgroups on each of 256 compute units
+// Two workgroups of four wavefronts on each of 256 compute units.  Blocks of 64 have three
+// or four of two wavefronts there, but their lists are cut no finer.
+constexpr int kPlaces = 512;
 constexpr int kFront = 2 * kPlaces;     // parts at most: c > limit makes less than c / limit + 1
 constexpr int kLeast = 2;               // shortest part, in list entries
 constexpr int kStaged = 8192;           // counts that the plan keeps in LDS
@@ -341,8 +343,11 @@ __global__ __launch_bounds__(1024) void bwd_plan_kernel(BwdArgs a, PlanSide rows
 
 // Rows of a walked tile of the query kernel.  Workgroups of two wavefronts take half at
 // d = 128, where that puts three of them on a compute unit instead of two (12 heads x
-// 16000 tokens, blocks of 64: 1011 -> 858 us); at d = 64 four of them fit with whole
-// tiles, and halves cost 3-11 %.
+// 16000 tokens, blocks of 64: 1011 -> 858 us).  At d = 64 whole tiles let four on it, and
+// halves of the query side alone, whose LDS is a union with the key side's, no more: 2 x 10
+// heads x 4000 tokens, blocks of 64, 106.5 and 110.8 us, 12 x 32760 925 and 948.  Halves of
+// both sides make three wavefronts a SIMD of two, for 107.6 and 105.0, 916 and 890, but with
+// 128 x 64 blocks 150 and 168 (12 x 8000).
 template <int BQ, int D>
 constexpr int kWalk = BQ == 64 && D == 128 ? 32 : 64;
 

@@ -299,6 +299,8 @@ __device__ __forceinline__ void attend(const DecodeArgs& a, int b, int h, int hg
     l_run *= alpha;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) o[i] *= alpha;
+    // the matrix product takes bf16: a probability is off by 2^-8 of itself there, as in the
+    // prompt's attention; the sum adds up the unrounded ones
     bf16x8 pf;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
