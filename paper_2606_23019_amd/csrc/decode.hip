@@ -164,9 +164,12 @@ __global__ __launch_bounds__(kDecodeSelectThreads) void decode_select_kernel(Dec
   const int b = bh / a.Hkv;
   const int n = (length_of(a, b) + a.blk - 1) / a.blk;  // blocks with a token
   int32_t* list = a.blocks + (int64_t)bh * a.topk;
-  for (int i = threadIdx.x; i < a.topk; i += kDecodeSelectThreads)
-    if (n <= a.topk) list[i] = i < n ? i : -1;
-  if (n <= a.topk) return;
+  if (n <= a.topk) {
+    // topk may be any int, so i may pass its end
+    for (uint32_t i = threadIdx.x; i < (uint32_t)a.topk; i += kDecodeSelectThreads)
+      list[i] = (int)i < n ? (int)i : -1;
+    return;
+  }
   const uint64_t* keys = a.keys + (int64_t)bh * a.n_blk;
   if (!a.keys) {
     score_blocks<D, kDecodeSelectThreads>(a, b, bh - b * a.Hkv, 0, n - 1, own_keys, lds);

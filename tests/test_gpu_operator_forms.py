@@ -159,3 +159,33 @@ def test_decode_in_one_launch_over_long_tables(case):
             assert blocks[b, h].tolist() == rb + [-1] * (topk - len(rb))
             check(out[b, rows], ro, eo)
             assert (np.abs(f64(lse[b, rows]) - rl) <= el).all()
+
+
+def test_decode_of_the_largest_topk():
+    """topk of 2^31 - 1 over a table of two blocks: the list is filled to its end, and what lies
+    around it stays as it was."""
+    import ctypes
+    import torch
+    from paper_2606_23019_amd import binding
+    P, topk, pad = ctypes.c_void_p, (1 << 31) - 1, 4096
+    g = gen(3)
+    q, k, v = randn(g, 1, 2, 64), randn(g, 1, 1, 100, 64), randn(g, 1, 1, 100, 64)
+    means = binding.block_means(k, 64)
+    ln = torch.tensor([99], device="cuda", dtype=torch.int32)
+    out, lse = torch.empty_like(q), torch.empty((1, 2), device="cuda")
+    room = torch.full((topk + 2 * pad,), 7, device="cuda", dtype=torch.int32)
+    blocks = room[pad:-pad]
+    lib = binding.load()
+    n = lib.sa_selected_decode_workspace(1, 2, 1, 100, 64, 64, topk)
+    ws = torch.empty(max(n, 1), device="cuda", dtype=torch.uint8)
+    strides = (ctypes.c_int64 * 3)(0, 0, 64)
+    assert lib.sa_selected_decode(P(q.data_ptr()), P(k.data_ptr()), P(v.data_ptr()), strides, P(means.data_ptr()),
+                                  P(ln.data_ptr()), P(out.data_ptr()), P(lse.data_ptr()), P(blocks.data_ptr()),
+                                  P(ws.data_ptr()), 1, 2, 1, 100, 64, 64, topk, 0.125, binding._stream(None)) == 0
+    torch.cuda.synchronize()
+    ro, rl, rb, eo, el = ops.selected_decode(f64(q[0]), f64(k[0, 0]), f64(v[0, 0]), f64(means[0, 0]), 99,
+                                             2, 64, 0.125, U16)
+    assert blocks[:2].tolist() == rb and bool((blocks[2:] == -1).all())
+    assert bool((room[:pad] == 7).all()) and bool((room[-pad:] == 7).all())
+    check(out[0], ro, eo)
+    assert (np.abs(f64(lse[0]) - rl) <= el).all()
