@@ -84,6 +84,7 @@ int rope_args(const void* q, const int64_t* q_strides, const void* k, const int6
   // a token's group and a run of heads are one workgroup's quarter at least
   if ((int64_t)B * N >= ((int64_t)1 << 31) || cdiv((int64_t)B * N, 16) * ((int64_t)Hq + Hk) > kMaxInt)
     return SA_ERR_UNSUPPORTED;
+  if (Hq > (1 << 30) || Hk > (1 << 30)) return SA_ERR_UNSUPPORTED;  // a run of heads ends past H
   size_t q_bytes, k_bytes;
   if (!strided(q_strides, {B, N, Hq}, d, &q_bytes) || !strided(k_strides, {B, N, Hk}, d, &k_bytes))
     return SA_ERR_INVALID_ARG;

@@ -74,3 +74,18 @@ def test_binding_refuses_sizes_beyond_32_bits():
     cos = torch.zeros((1, 32)).expand((1 << 32) + 1, 32)
     with pytest.raises(ValueError, match="cos and sin have"):
         binding._rope_shapes(row, row, w, w, cos, cos, torch.zeros((1, 1)).int(), "halves", "bhnd")
+
+
+def test_norm_and_rotation_of_more_heads_than_a_kernel_counts(lib):
+    # a run of heads ends up to 16 past H, in an int
+    def call(Hq, Hk, bwd):
+        a = [binding.ctypes.c_void_p(i << 44) for i in range(1, 15)]
+        s = strides(0, 0, 0)
+        tail = (1, 1, Hq, Hk, 64, 64, 1, 1e-6, 0, 0, None)
+        if bwd:
+            return lib.sa_qk_norm_rope_bwd(a[0], a[1], a[2], s, a[3], s, a[4], a[5], a[6], a[7], None, a[8], a[9],
+                                           a[10], a[11], a[12], *tail)
+        return lib.sa_qk_norm_rope(a[0], s, a[1], s, a[2], a[3], a[4], a[5], None, a[6], a[7], *tail)
+    for bwd in (False, True):
+        for heads in ((1 << 30) + 1, (1 << 31) - 2):
+            assert call(heads, 1, bwd) == UNSUPPORTED and call(1, heads, bwd) == UNSUPPORTED
