@@ -25,8 +25,10 @@
 // density about 0.13): 2.69-2.75 ms, 7 products at 1.10-1.13 PFLOP/s (the forward kernel
 // 1.05-1.1; a large library product 1.16-1.35, depending on the card); the 5 that the
 // formulas need would take 1.6-1.9 ms at the library's rate.  2 x 10 heads x 4000 tokens
-// (d = 64, blocks of 64): 108 us, of which 95-100 in the two kernels at 0.75-0.79 PFLOP/s:
-// there the exponentials take as long as the products.
+// (d = 64, blocks of 64): 106 us, of which 97-100 in the two kernels at 0.75-0.77 PFLOP/s:
+// there compute units are busy for 74 % of the cycles (the start, and an end that the longest
+// lists draw out), and while they are, the matrix cores are for 45 % and the vector ALU for
+// 42 %, which two wavefronts a SIMD overlap little of.
 
 #include <math.h>
 

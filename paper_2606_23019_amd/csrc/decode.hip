@@ -15,11 +15,11 @@
 //
 // Bound: HBM bytes of the means and of the chosen blocks' keys and values, which are
 // read once for the whole group; with few rows the latency of the launches.  Measured:
-// 16 sequences of up to 135000 tokens, 8 key heads, 64 blocks of 128: 104 us, 5.5 TB/s in
-// all, of which selection 22 (one compute unit a row) and attention about 80 (a reduction
-// reads at 5.7 TB/s); 2 x 12 heads, 16 blocks of 64: 17 us a call, where what one
-// compute unit reads of its row's 0.5 MB bounds it (twice the loads in flight change
-// nothing).
+// 16 sequences of up to 135000 tokens, 8 key heads, 64 blocks of 128: 103 us, 5.6 TB/s in
+// all (2 GiB past the caches are read at 7.1); by themselves the selection takes 18 (one
+// compute unit a row), the attention 90 and the join 5; 2 x 12 heads, 16 blocks of 64:
+// 16 us a call, where what one compute unit reads of its row's 0.5 MB bounds it (twice the
+// loads in flight change nothing).
 
 #include <math.h>
 

@@ -16,9 +16,9 @@
 //
 // Bound: HBM bytes (4 an element forward, 6 backward; some 20 vector instructions
 // for every 8 elements).  Everything is fp32; each output is rounded to bf16 once.
-// Measured: 75600 tokens x 80 heads of 128 in 566 us, 5.5 TB/s (a 2 GiB copy runs at
-// 4.85); gradients of 2 x 32760 tokens x 24 heads in 235 us, 5.2 TB/s.  Eight tokens
-// take 4 us on the GPU and 15 us a call, the host's part.
+// Measured: 75600 tokens x 80 heads of 128 in 566 us, 5.5 TB/s (a copy of 2 GiB past the
+// caches runs at 6.1); gradients of 2 x 32760 tokens x 24 heads in 224 us, 5.5 TB/s.  Eight
+// tokens take 4 us on the GPU and 14 us a call, the host's part.
 
 #include <type_traits>
 

@@ -9,11 +9,11 @@
 // sums nor an fp32 rounding decides between two blocks.  A mean is the fp32 rounding
 // of the 64-bit sum's quotient, a score the 64-bit sum of exact products.
 //
-// Measured, 40 heads x 75600 tokens (591 x 591 blocks of 128, d = 128): means about 112 us
-// a tensor, 6.9 TB/s (a reduction over 2 GiB reads at 5.7); selection of 59 with kept
-// blocks and candidates that leave half of the tiles 115-125 us (all of them 145-150: the
-// products' 3.6 Gflop take some 75, 56 at the 64 TFLOP/s of a large 64-bit matrix
-// product, the borders 18).
+// Measured, 40 heads x 75600 tokens (591 x 591 blocks of 128, d = 128): means 113-118 us a
+// tensor, 6.6-6.9 TB/s (2 GiB past the caches are read at 7.1); selection of 59 with kept
+// blocks 122 us, 121-125 with candidates that leave half of the tiles (their bits cost what
+// the skipped tiles save; scored all the same they took 145-150).  The products' 3.6 Gflop
+// would take 54 at the 67 TFLOP/s of a large 64-bit matrix product.
 
 #include <type_traits>
 
